@@ -1,0 +1,419 @@
+"""The operators that generate from a compressed prompt, and what they are measured on.
+
+A case is one pass through one of them.  Its `kind`:
+
+  rope    a prompt's queries and keys as a fused projection wrote them (token by
+          token, queries, keys and values of a token side by side) get their
+          per-head norms and rotary positions; the window's queries are also
+          written where the eviction pass reads them;
+  append  the tokens that continue compressed prompts: norm and rotation of the
+          new queries and keys, and the new rows' places in the paged tails;
+  shared  one generated token of every continuation: attention over the prompt's
+          kept rows, which its continuations share, and over its own paged tail.
+
+Every drawn value is N(0, 1); keys and queries of `shared` have an offset in
+common, as the keys of real prompts do.
+"""
+import math
+
+import torch
+
+own = False
+
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def listed():
+    return [
+        # one long prompt of one layer, as the prefill meets it: plain half-split rotary positions
+        {"name": "rope_prompt_32k", "kind": "rope", "dtype": "bf16", "layers": 1, "q_heads": 28, "kv_heads": 4, "dim": 128,
+         "lens": "32768", "rot": 128, "pairs": "half", "norm": False, "stretch": 1.0, "window": 4, "far": 0},
+        # packed ragged prompts of a model that normalises queries and keys, its positions stretched
+        {"name": "rope_packed_norm", "kind": "rope", "dtype": "bf16", "layers": 1, "q_heads": 32, "kv_heads": 8, "dim": 128,
+         "lens": "4133,977,8201,33,2050", "rot": 128, "pairs": "interleaved", "norm": True, "stretch": 4.0, "window": 8, "far": 0},
+        # a few layers of a small fp32 model that rotates half of each head, far into a long text
+        {"name": "rope_partial_f32", "kind": "rope", "dtype": "f32", "layers": 2, "q_heads": 8, "kv_heads": 4, "dim": 64,
+         "lens": "509,130", "rot": 32, "pairs": "half", "norm": False, "stretch": 1.0, "window": 8, "far": 900001},
+        # the smallest call: one token of one continuation in one layer
+        {"name": "append_one", "kind": "append", "dtype": "bf16", "layers": 1, "q_heads": 28, "kv_heads": 4, "dim": 128,
+         "tokens": "1", "rot": 128, "pairs": "half", "norm": False, "stretch": 1.0, "tail": 200, "page": 16},
+        # one token of each of 48 continuations in one layer, with norms
+        {"name": "append_batch", "kind": "append", "dtype": "bf16", "layers": 1, "q_heads": 32, "kv_heads": 8, "dim": 128,
+         "tokens": ",".join(["1"] * 48), "rot": 128, "pairs": "half", "norm": True, "stretch": 1.0, "tail": 1000, "page": 64},
+        # follow-up questions of odd lengths appended whole
+        {"name": "append_chunks", "kind": "append", "dtype": "bf16", "layers": 1, "q_heads": 28, "kv_heads": 4, "dim": 128,
+         "tokens": "513,77,1,1030,260,999,31,641", "rot": 64, "pairs": "interleaved", "norm": False, "stretch": 8.0, "tail": 300,
+         "page": 64},
+        # two continuations of a tiny fp32 prompt: launches and host work are all there is
+        {"name": "shared_tiny_f32", "kind": "shared", "dtype": "f32", "layers": 1, "q_heads": 2, "kv_heads": 2, "dim": 128,
+         "kept": "128", "fan": "2", "ragged": False, "tail": 5, "page": 16},
+        # eight answers to one compressed prompt, one layer: the call that every token makes in every layer
+        {"name": "shared_layer_8", "kind": "shared", "dtype": "bf16", "layers": 1, "q_heads": 28, "kv_heads": 4, "dim": 128,
+         "kept": "6553", "fan": "8", "ragged": False, "tail": 200, "page": 64},
+        # many continuations with long tails
+        {"name": "shared_layer_64", "kind": "shared", "dtype": "bf16", "layers": 1, "q_heads": 28, "kv_heads": 4, "dim": 128,
+         "kept": "6553", "fan": "64", "ragged": False, "tail": 777, "page": 64},
+        # several prompts whose heads kept different numbers of rows, continued by different numbers of answers
+        {"name": "shared_prompts", "kind": "shared", "dtype": "bf16", "layers": 1, "q_heads": 32, "kv_heads": 8, "dim": 128,
+         "kept": "4480,619,2610,4800,1358", "fan": "5,1,12,0,3", "ragged": True, "tail": 333, "page": 16},
+        # 64-wide heads that are not grouped, a long prompt
+        {"name": "shared_mha_d64", "kind": "shared", "dtype": "bf16", "layers": 2, "q_heads": 32, "kv_heads": 32, "dim": 64,
+         "kept": "8191", "fan": "20", "ragged": False, "tail": 100, "page": 128},
+        # the whole model's compressed cache in one call
+        {"name": "shared_stack28", "kind": "shared", "dtype": "bf16", "layers": 28, "q_heads": 28, "kv_heads": 4, "dim": 128,
+         "kept": "6553", "fan": "16", "ragged": False, "tail": 130, "page": 64},
+    ]
+
+
+# (query heads, KV heads) of the drawn cases
+HEADS = [(28, 4), (32, 8), (16, 2), (8, 4), (32, 32), (2, 2)]
+
+
+def _spread(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _texts(numbers):
+    return ",".join(map(str, numbers))
+
+
+def draw(rng):
+    kind = rng.choice(["rope", "append", "shared", "shared"])
+    q_heads, kv_heads = rng.choice(HEADS)
+    case = {"kind": kind, "dtype": rng.choice(["bf16", "bf16", "bf16", "f32"]), "layers": 1, "q_heads": q_heads,
+            "kv_heads": kv_heads, "dim": rng.choice([128, 128, 64])}
+    if kind == "shared":
+        kept = [_spread(rng, 64, 8192) for _ in range(rng.choice([1, 1, 1, 2, 5]))]
+        fan = [_spread(rng, 1, 64) for _ in kept]
+        tail = _spread(rng, 1, 1024)
+        if case["dtype"] == "f32":  # for small models and checks
+            kept, fan = [min(n, 2048) for n in kept], [min(n, 8) for n in fan]
+        # no more rows, and no more products, than the largest listed case
+        rows = kv_heads * (sum(kept) + sum(fan) * tail)
+        products = q_heads * sum(n * f for n, f in zip(kept, fan))
+        most = min(28 * 4 * (6553 + 16 * 130) // rows, 28 * 28 * 6553 * 16 // products, 28)
+        while most < 1:
+            kept, fan, tail = [max(1, n // 2) for n in kept], [max(1, n // 2) for n in fan], max(1, tail // 2)
+            rows = kv_heads * (sum(kept) + sum(fan) * tail)
+            products = q_heads * sum(n * f for n, f in zip(kept, fan))
+            most = min(28 * 4 * (6553 + 16 * 130) // rows, 28 * 28 * 6553 * 16 // products, 28)
+        case.update(layers=_spread(rng, 1, most), kept=_texts(kept), fan=_texts(fan), ragged=rng.random() < 0.4, tail=tail,
+                    page=rng.choice([1, 16, 16, 64, 256]))
+        return case
+    case.update(rot=rng.choice([case["dim"], case["dim"], case["dim"] // 2, 16]), pairs=rng.choice(["half", "half", "interleaved"]),
+                norm=rng.random() < 0.4, stretch=rng.choice([1.0, 1.0, 4.0, 16.0]))
+    if kind == "rope":
+        lens = [_spread(rng, 16, 8192) for _ in range(rng.choice([1, 1, 2, 5]))]
+        case.update(lens=_texts(lens), layers=_spread(rng, 1, max(1, min(8, 24000 // sum(lens)))), window=rng.choice([4, 8, 16]),
+                    far=rng.choice([0, 0, 131071]))
+    else:
+        tokens = [rng.choice([1, 1, _spread(rng, 1, 600)]) for _ in range(_spread(rng, 1, 64))]
+        case.update(tokens=_texts(tokens), tail=_spread(rng, 1, 1024), page=rng.choice([1, 16, 16, 64, 256]))
+    return case
+
+
+# ---------------------------------------------------------------------------
+
+def _ints(text):
+    return [int(v) for v in str(text).split(",")]
+
+
+def _generator(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _normal(g, shape, dtype):
+    return torch.randn(shape, generator=g, device="cuda").to(dtype)
+
+
+def _int32(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def _tails(case, seed, conts, rows):
+    """Pages enough for `rows` rows of every continuation, dealt out in a random order."""
+    page = case["page"]
+    per = -(-rows // page)
+    order = torch.randperm(conts * per + 3, generator=torch.Generator().manual_seed(seed))
+    return per, conts * per + 3, order[:conts * per].view(conts, per).to(torch.int32).cuda()
+
+
+def _rope(case, g):
+    """Rotation frequencies: base 10000, the slow ones divided by `stretch` with a ramp between (32 and 1 turns within
+    4096 positions) and cosines and sines made larger by 0.1 ln(stretch) + 1; and the norms' weights."""
+    rot, k = case["rot"], case["stretch"]
+    i = torch.arange(rot // 2, dtype=torch.float64)
+    freq = 10000.0 ** (-2 * i / rot)
+    if k != 1.0:
+        turns = 4096 * freq / (2 * math.pi)
+        keep = ((turns - 1) / 31).clamp(0, 1)
+        freq = freq * (keep + (1 - keep) / k)
+    w = {n: (1 + 0.1 * _normal(g, (case["dim"],), torch.float32)).to(TYPES[case["dtype"]]) if case["norm"] else None for n in ("q_norm", "k_norm")}
+    return {"freq": freq.float().cuda(), "factor": 0.1 * math.log(k) + 1.0, "eps": 1e-6, **w}
+
+
+def _tail_rows(case, conts):
+    """Rows in the tails: between a half of the longest and the longest."""
+    t = case["tail"]
+    return [max(1, t - t * (7919 * c % 101) // 202) for c in range(conts)]
+
+
+def _kept_rows(case):
+    """[layers][kv_heads][prompts] kept rows: the budget, or more in some heads and fewer in others."""
+    f = lambda n, l, h, s: n if not case["ragged"] else max(1, n * (6 + (37 * h + 11 * l + 5 * s) % 9) // 10)  # noqa: E731
+    return [[[f(n, l, h, s) for s, n in enumerate(_ints(case["kept"]))] for h in range(case["kv_heads"])] for l in range(case["layers"])]
+
+
+def prepare(case, seed):
+    g, dtype = _generator(seed), TYPES[case["dtype"]]
+    L, Hq, Hkv, D = case["layers"], case["q_heads"], case["kv_heads"], case["dim"]
+    s = {"case": case}
+    if case["kind"] != "shared":
+        n = sum(_ints(case["lens" if case["kind"] == "rope" else "tokens"]))
+        qkv = _normal(g, (L, n, Hq + 2 * Hkv, D), dtype)
+        s.update(Q=qkv[:, :, :Hq], K=qkv[:, :, Hq:Hq + Hkv], V=qkv[:, :, Hq + Hkv:], rope=_rope(case, g))
+    if case["kind"] == "rope":
+        lens = _ints(case["lens"])
+        cu = [0]
+        for t in lens:
+            cu.append(cu[-1] + t)
+        s.update(cu=cu, positions=_int32([case["far"] + i for t in lens for i in range(t)]))
+        # where the window's rows of each prompt are among the packed tokens
+        s["window"] = torch.tensor([list(range(e - case["window"], e)) for e in cu[1:]], device="cuda")
+    elif case["kind"] == "append":
+        tokens = _ints(case["tokens"])
+        start = [t - 1 for t in _tail_rows(case, len(tokens))]
+        per, pages, s["table"] = _tails(case, seed, len(tokens), max(a + t for a, t in zip(start, tokens)))
+        s["conts"] = _int32([c for c, t in enumerate(tokens) for _ in range(t)])
+        s["rows"] = _int32([a + j for a, t in zip(start, tokens) for j in range(t)])
+        s["positions"] = _int32([5000 + 37 * c + a + j for c, (a, t) in enumerate(zip(start, tokens)) for j in range(t)])
+        s["tail_K"], s["tail_V"] = (_normal(g, (L, pages, Hkv, case["page"], D), dtype) for _ in range(2))
+    else:
+        fan, kept = _ints(case["fan"]), _kept_rows(case)
+        N = sum(fan)
+        off = torch.randn((L, Hkv, 1, D), generator=g, device="cuda")
+        counts = torch.tensor(kept).view(-1)
+        s["counts"] = counts.to(torch.int32).cuda()
+        s["offsets"] = (counts.cumsum(0) - counts).to(torch.int32).cuda()
+        s["first"] = [0]
+        for f in fan:
+            s["first"].append(s["first"][-1] + f)
+        own_head = torch.repeat_interleave(torch.arange(L * Hkv), torch.tensor(kept).sum(2).view(-1)).cuda()
+        s["Kc"] = (torch.randn((own_head.numel(), D), generator=g, device="cuda") + off.view(-1, D)[own_head]).to(dtype)
+        s["Vc"] = _normal(g, (own_head.numel(), D), dtype)
+        q = torch.randn((L, Hkv, Hq // Hkv, N, D), generator=g, device="cuda") + off[:, :, None]
+        s["Q"] = q.view(L, Hq, N, D).to(dtype)
+        tails = _tail_rows(case, N)
+        per, pages, s["table"] = _tails(case, seed, N, max(tails))
+        s["tail_counts"] = _int32(tails)
+        s["tail_K"] = (torch.randn((L, pages, Hkv, case["page"], D), generator=g, device="cuda") + off[:, None]).to(dtype)
+        s["tail_V"] = _normal(g, (L, pages, Hkv, case["page"], D), dtype)
+    return s
+
+
+# ---------------------------------------------------------------------------
+# The operators in elementary steps.
+
+def _turned(s, x, positions, weight):
+    """Norm and rotation of rows [L][n][H][D] at positions [n], in float32."""
+    case, rope = s["case"], s["rope"]
+    x = x.float()
+    if weight is not None:
+        x = x * torch.rsqrt((x * x).mean(-1, keepdim=True) + rope["eps"]) * weight.float()
+    angle = positions.double()[:, None] * rope["freq"].double()
+    c, d = ((rope["factor"] * f(angle)).float()[None, :, None, :] for f in (torch.cos, torch.sin))
+    rot = case["rot"]
+    t = x[..., :rot]
+    if case["pairs"] == "half":
+        a, b = t[..., :rot // 2], t[..., rot // 2:]
+        t = torch.cat([a * c - b * d, b * c + a * d], dim=-1)
+    else:
+        a, b = t[..., 0::2], t[..., 1::2]
+        t = torch.stack([a * c - b * d, b * c + a * d], dim=-1).flatten(-2)
+    return torch.cat([t, x[..., rot:]], dim=-1)
+
+
+def _plain_rope(s):
+    dtype = s["Q"].dtype
+    q = _turned(s, s["Q"], s["positions"], s["rope"]["q_norm"]).to(dtype)
+    k = _turned(s, s["K"], s["positions"], s["rope"]["k_norm"]).to(dtype)
+    win = q[:, s["window"]].permute(0, 3, 1, 2, 4).contiguous()  # [L][B][w][Hq][D] -> [L][Hq][B][w][D]
+    return {"Q": q, "K": k, "Q_win": win}
+
+
+def _plain_append(s):
+    page, dtype = s["case"]["page"], s["Q"].dtype
+    q = _turned(s, s["Q"], s["positions"], s["rope"]["q_norm"]).to(dtype).transpose(1, 2).contiguous()
+    k = _turned(s, s["K"], s["positions"], s["rope"]["k_norm"]).to(dtype)
+    row = s["rows"].long()
+    at, in_page = s["table"][s["conts"].long(), row // page].long(), row % page
+    s["tail_K"].permute(1, 3, 0, 2, 4)[at, in_page] = k.transpose(0, 1)
+    s["tail_V"].permute(1, 3, 0, 2, 4)[at, in_page] = s["V"].transpose(0, 1)
+    return {"Q": q, "tail_K": s["tail_K"], "tail_V": s["tail_V"]}
+
+
+def _plain_shared(s):
+    case = s["case"]
+    L, Hq, Hkv, D, page = case["layers"], case["q_heads"], case["kv_heads"], case["dim"], case["page"]
+    G, N = Hq // Hkv, s["Q"].shape[2]
+    first = torch.tensor(s["first"])
+    B, fan = len(first) - 1, first.diff()
+    # the prompts' rows [L][Hkv][B][most][D] and their continuations [B][F], padded to the largest
+    counts, offsets = (s[n].long().view(L, Hkv, B, 1) for n in ("counts", "offsets"))
+    j = torch.arange(max(n for l in _kept_rows(case) for h in l for n in h), device="cuda")
+    rows = (offsets + torch.minimum(j, counts - 1)).view(-1)
+    f = torch.arange(int(fan.max()))
+    member = torch.minimum(first[:-1, None] + f, (first[1:, None] - 1).clamp_min(0)).cuda()
+    q = s["Q"].float().view(L, Hkv, G, N, D)
+    qb = q[:, :, :, member].permute(0, 1, 3, 4, 2, 5).reshape(L * Hkv * B, -1, D)
+    Kp, Vp = (s[n][rows].float().view(L * Hkv * B, -1, D) for n in ("Kc", "Vc"))
+    x = torch.bmm(qb, Kp.transpose(1, 2).contiguous()) / math.sqrt(D)
+    x.masked_fill_((j >= counts).view(L * Hkv * B, 1, -1), -math.inf)
+    # the tails' rows [L][Hkv][N][longest][D]
+    j = torch.arange(max(_tail_rows(case, N)), device="cuda")
+    at = s["table"].long()[:, j // page]
+    Kt, Vt = (s[n].permute(1, 3, 0, 2, 4)[at, (j % page).expand_as(at)].float().permute(2, 3, 0, 1, 4).reshape(L * Hkv * N, -1, D) for n in ("tail_K", "tail_V"))
+    y = torch.bmm(q.transpose(2, 3).reshape(L * Hkv * N, G, D), Kt.transpose(1, 2).contiguous()) / math.sqrt(D)
+    y.view(L, Hkv, N, G, -1).masked_fill_((j >= s["tail_counts"].long()[:, None])[None, None, :, None], -math.inf)
+    # one softmax over both: the prompt's part goes from [B][F] places to continuations
+    place = torch.repeat_interleave(torch.arange(B), fan) * int(fan.max()) + torch.cat([torch.arange(int(n)) for n in fan])
+    place = place.cuda()
+    m = torch.maximum(x.amax(-1).view(L, Hkv, -1, G)[:, :, place], y.amax(-1).view(L, Hkv, N, G))
+    mb = torch.zeros((L, Hkv, B * int(fan.max()), G), device="cuda")
+    mb[:, :, place] = m
+    x = torch.exp(x - mb.view(L * Hkv * B, -1, 1))
+    y = torch.exp(y - m.view(L * Hkv * N, G, 1))
+    z = x.sum(-1).view(L, Hkv, -1, G)[:, :, place] + y.sum(-1).view(L, Hkv, N, G)
+    o = torch.bmm(x, Vp).view(L, Hkv, -1, G, D)[:, :, place] + torch.bmm(y, Vt).view(L, Hkv, N, G, D)
+    O = (o / z[..., None]).transpose(2, 3).reshape(L, Hq, N, D)
+    return {"O": O, "lse": (m + torch.log(z)).transpose(2, 3).reshape(L, Hq, N)}
+
+
+# ---------------------------------------------------------------------------
+# The same through the library.
+
+def _kept(s):
+    """What a program holds beside its inputs: shape, handles, outputs and workspace, made on a state's first pass."""
+    import paper_2609_06663_amd as P
+    case = s["case"]
+    L, Hq, Hkv, D, dtype = case["layers"], case["q_heads"], case["kv_heads"], case["dim"], s["Q"].dtype
+    k = s["kept"] = {"P": P}
+    empty = lambda *shape, dtype=dtype: torch.empty(shape, dtype=dtype, device="cuda")  # noqa: E731
+    if case["kind"] == "rope":
+        k["shape"] = P.Shape(L, Hq, Hkv, D, case["window"], s["cu"])
+        k.update(Q=empty(L, s["cu"][-1], Hq, D), K=empty(L, s["cu"][-1], Hkv, D), Q_win=empty(L, Hq, len(s["cu"]) - 1, case["window"], D))
+    elif case["kind"] == "append":
+        k["shape"] = P.Shape(L, Hq, Hkv, D, 4, [0, 5000])
+        k["Q"] = empty(L, Hq, s["rows"].numel(), D)
+    else:
+        kept = _kept_rows(case)
+        cu = [0]
+        for n in _ints(case["kept"]):  # the prompts were five times as long as what their heads kept
+            cu.append(cu[-1] + 5 * n + 4)
+        N = s["Q"].shape[2]
+        k.update(shape=P.Shape(L, Hq, Hkv, D, 4, cu), max_count=max(n for l in kept for h in l for n in h),
+                 max_tail=max(_tail_rows(case, N)), O=empty(L, Hq, N, D, dtype=torch.float32), lse=empty(L, Hq, N, dtype=torch.float32))
+        k["ws"] = empty(max(256, P.ecokv_decode_shared_workspace_size(k["shape"], s["first"], k["max_count"], k["max_tail"])), dtype=torch.uint8)
+    if case["kind"] != "shared":
+        r = s["rope"]
+        k["rope"] = P.Rope(case["rot"], r["freq"], interleaved=case["pairs"] == "interleaved", factor=r["factor"], q_norm=r["q_norm"],
+                           k_norm=r["k_norm"], norm_eps=r["eps"])
+    if case["kind"] != "rope":
+        k["tails"] = P.Tails(s["tail_K"], s["tail_V"], s["table"])
+    return k
+
+
+def run(s):
+    kind = s["case"]["kind"]
+    if not own:
+        return {"rope": _plain_rope, "append": _plain_append, "shared": _plain_shared}[kind](s)
+    k = s.get("kept") or _kept(s)
+    P = k["P"]
+    if kind == "rope":
+        P.ecokv_prefill_rope(s["Q"], s["K"], k["shape"], k["rope"], s["positions"], k["Q"], k["K"], k["Q_win"])
+        return {"Q": k["Q"], "K": k["K"], "Q_win": k["Q_win"]}
+    if kind == "append":
+        P.ecokv_append(s["Q"], s["K"], s["V"], k["shape"], k["rope"], s["positions"], s["conts"], s["rows"], k["tails"], k["Q"])
+        return {"Q": k["Q"], "tail_K": s["tail_K"], "tail_V": s["tail_V"]}
+    P.ecokv_decode_shared(s["Q"], s["Kc"], s["Vc"], k["shape"], s["first"], s["counts"], s["offsets"], k["max_count"], k["tails"],
+                          s["tail_counts"], k["max_tail"], k["O"], k["lse"], k["ws"])
+    return {"O": k["O"], "lse": k["lse"]}
+
+
+# ---------------------------------------------------------------------------
+
+def work(case):
+    L, Hq, Hkv, D = case["layers"], case["q_heads"], case["kv_heads"], case["dim"]
+    row = D * (2 if case["dtype"] == "bf16" else 4)
+    if case["kind"] == "rope":
+        lens = _ints(case["lens"])
+        rows = L * sum(lens) * (Hq + Hkv)
+        return {"bytes": 2 * rows * row + L * Hq * len(lens) * case["window"] * row + 4 * sum(lens), "flops": rows * (4 * D if case["norm"] else 0) + rows * 3 * case["rot"]}
+    if case["kind"] == "append":
+        n = sum(_ints(case["tokens"]))
+        rows = L * n * (Hq + Hkv)
+        return {"bytes": 2 * (rows + L * n * Hkv) * row + 12 * n, "flops": rows * (4 * D if case["norm"] else 0) + rows * 3 * case["rot"]}
+    fan, G = _ints(case["fan"]), Hq // Hkv
+    N = sum(fan)
+    kept = [sum(h[s] for l in _kept_rows(case) for h in l) for s in range(len(fan))]
+    tail = L * Hkv * sum(_tail_rows(case, N))
+    used = sum(n for n, f in zip(kept, fan) if f)  # the rows of a prompt that nobody continues are not read
+    return {"bytes": 2 * (used + tail) * row + L * Hq * N * (row + 4 * D + 4), "flops": 4 * D * G * (sum(n * f for n, f in zip(kept, fan)) + tail)}
+
+
+# ---------------------------------------------------------------------------
+# The definitions in 64 bits.
+
+def _turn64(x, positions, case, rope, weight):
+    x = x.double()
+    if weight is not None:
+        x = x / torch.sqrt(x.pow(2).sum(-1, keepdim=True) / case["dim"] + rope["eps"]) * weight.double()
+    half, out = case["rot"] // 2, x.clone()
+    for i in range(half):  # pair by pair: a rotation in the plane of two dimensions
+        a, b = (i, i + half) if case["pairs"] == "half" else (2 * i, 2 * i + 1)
+        theta = (positions.double() * float(rope["freq"][i]))[None, :, None]
+        z = torch.complex(x[..., a], x[..., b]) * torch.polar(torch.full_like(theta, rope["factor"]), theta)
+        out[..., a], out[..., b] = z.real, z.imag
+    return out
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    L, Hq, Hkv, D = case["layers"], case["q_heads"], case["kv_heads"], case["dim"]
+    G = Hq // Hkv
+    if case["kind"] != "shared":
+        q = _turn64(s["Q"], s["positions"], case, s["rope"], s["rope"]["q_norm"])
+        k = _turn64(s["K"], s["positions"], case, s["rope"], s["rope"]["k_norm"])
+    if case["kind"] == "rope":
+        w = case["window"]
+        win = torch.stack([q[:, e - w:e].transpose(1, 2) for e in s["cu"][1:]], dim=2)
+        return {"Q": q, "K": k, "Q_win": win}
+    page = case["page"]
+    if case["kind"] == "append":
+        tk, tv = s["tail_K"].double(), s["tail_V"].double()
+        for t, (c, r) in enumerate(zip(s["conts"].tolist(), s["rows"].tolist())):
+            p = int(s["table"][c, r // page])
+            tk[:, p, :, r % page] = k[:, t]
+            tv[:, p, :, r % page] = s["V"][:, t].double()
+        return {"Q": q.transpose(1, 2), "tail_K": tk, "tail_V": tv}
+    N = s["Q"].shape[2]
+    O = torch.empty((L, Hq, N, D), dtype=torch.float64, device="cuda")
+    lse = torch.empty((L, Hq, N), dtype=torch.float64, device="cuda")
+    counts, offsets, tails = s["counts"].tolist(), s["offsets"].tolist(), s["tail_counts"].tolist()
+    B = len(s["first"]) - 1
+    parent = [b for b in range(B) for _ in range(s["first"][b], s["first"][b + 1])]
+    for l in range(L):
+        for h in range(Hkv):
+            for c in range(N):
+                u = (l * Hkv + h) * B + parent[c]
+                at, n = offsets[u], tails[c]
+                pages = s["table"][c, :-(-n // page)].long()
+                K, V = (torch.cat([s[p][at:at + counts[u]].double(), s[t][l, pages, h].reshape(-1, D)[:n].double()]) for p, t in (("Kc", "tail_K"), ("Vc", "tail_V")))
+                x = K @ s["Q"][l, h * G:(h + 1) * G, c].double().t() / math.sqrt(D)
+                top = x.max(dim=0).values
+                e = torch.exp(x - top)
+                O[l, h * G:(h + 1) * G, c] = (e.t() @ V) / e.sum(dim=0)[:, None]
+                lse[l, h * G:(h + 1) * G, c] = top + torch.log(e.sum(dim=0))
+    return {"O": O, "lse": lse}
