@@ -88,17 +88,14 @@ def draw(rng):
         tail = _spread(rng, 1, 1024)
         if case["dtype"] == "f32":  # for small models and checks
             kept, fan = [min(n, 2048) for n in kept], [min(n, 8) for n in fan]
-        # no more rows, and no more products, than the largest listed case
-        rows = kv_heads * (sum(kept) + sum(fan) * tail)
-        products = q_heads * sum(n * f for n, f in zip(kept, fan))
-        most = min(28 * 4 * (6553 + 16 * 130) // rows, 28 * 28 * 6553 * 16 // products, 28)
-        while most < 1:
+        case.update(kept="", fan="", ragged=rng.random() < 0.4, tail=tail, page=rng.choice([1, 16, 16, 64, 256]))
+        top, share = work(listed()[-1]), 0
+        while share < 1:  # no more bytes, and no more products, than the largest listed case
+            case.update(kept=_texts(kept), fan=_texts(fan), tail=tail)
+            one = work(case)
+            share = int(min(28, *(top[k] / one[k] for k in top)))
             kept, fan, tail = [max(1, n // 2) for n in kept], [max(1, n // 2) for n in fan], max(1, tail // 2)
-            rows = kv_heads * (sum(kept) + sum(fan) * tail)
-            products = q_heads * sum(n * f for n, f in zip(kept, fan))
-            most = min(28 * 4 * (6553 + 16 * 130) // rows, 28 * 28 * 6553 * 16 // products, 28)
-        case.update(layers=_spread(rng, 1, most), kept=_texts(kept), fan=_texts(fan), ragged=rng.random() < 0.4, tail=tail,
-                    page=rng.choice([1, 16, 16, 64, 256]))
+        case["layers"] = _spread(rng, 1, share)
         return case
     case.update(rot=rng.choice([case["dim"], case["dim"], case["dim"] // 2, 16]), pairs=rng.choice(["half", "half", "interleaved"]),
                 norm=rng.random() < 0.4, stretch=rng.choice([1.0, 1.0, 4.0, 16.0]))
