@@ -88,24 +88,26 @@ def draw(rng):
         tail = _spread(rng, 1, 1024)
         if case["dtype"] == "f32":  # for small models and checks
             kept, fan = [min(n, 2048) for n in kept], [min(n, 8) for n in fan]
-        case.update(kept="", fan="", ragged=rng.random() < 0.4, tail=tail, page=rng.choice([1, 16, 16, 64, 256]))
-        top, share = work(listed()[-1]), 0
-        while share < 1:  # no more bytes, and no more products, than the largest listed case
-            case.update(kept=_texts(kept), fan=_texts(fan), tail=tail)
-            one = work(case)
-            share = int(min(28, *(top[k] / one[k] for k in top)))
-            kept, fan, tail = [max(1, n // 2) for n in kept], [max(1, n // 2) for n in fan], max(1, tail // 2)
-        case["layers"] = _spread(rng, 1, share)
-        return case
-    case.update(rot=rng.choice([case["dim"], case["dim"], case["dim"] // 2, 16]), pairs=rng.choice(["half", "half", "interleaved"]),
-                norm=rng.random() < 0.4, stretch=rng.choice([1.0, 1.0, 4.0, 16.0]))
-    if kind == "rope":
-        lens = [_spread(rng, 16, 8192) for _ in range(rng.choice([1, 1, 2, 5]))]
-        case.update(lens=_texts(lens), layers=_spread(rng, 1, max(1, min(8, 24000 // sum(lens)))), window=rng.choice([4, 8, 16]),
-                    far=rng.choice([0, 0, 131071]))
+        case.update(ragged=rng.random() < 0.4, page=rng.choice([1, 16, 16, 64, 256]))
+        sizes = {"kept": kept, "fan": fan, "tail": tail}
     else:
-        tokens = [rng.choice([1, 1, _spread(rng, 1, 600)]) for _ in range(_spread(rng, 1, 64))]
-        case.update(tokens=_texts(tokens), tail=_spread(rng, 1, 1024), page=rng.choice([1, 16, 16, 64, 256]))
+        case.update(rot=rng.choice([case["dim"], case["dim"], case["dim"] // 2, 16]), pairs=rng.choice(["half", "half", "interleaved"]),
+                    norm=rng.random() < 0.4, stretch=rng.choice([1.0, 1.0, 4.0, 16.0]))
+        if kind == "rope":
+            case.update(window=rng.choice([4, 8, 16]), far=rng.choice([0, 0, 131071]))
+            sizes = {"lens": [_spread(rng, 32, 16384) for _ in range(rng.choice([1, 1, 2, 5]))]}
+        else:
+            case.update(tail=_spread(rng, 1, 1024), page=rng.choice([1, 16, 16, 64, 256]))
+            sizes = {"tokens": [rng.choice([1, 1, _spread(rng, 1, 600)]) for _ in range(_spread(rng, 1, 64))]}
+    # no more bytes, and no more products, than the largest listed case
+    top, share = work(listed()[-1]), 0
+    while share < 1:
+        case.update({k: _texts(v) if isinstance(v, list) else v for k, v in sizes.items()})
+        one = work(case)
+        share = int(min(28, *(top[k] / one[k] for k in top if one[k])))
+        floor = case.get("window", 1)
+        sizes = {k: [max(floor, n // 2) for n in v] if isinstance(v, list) else max(1, v // 2) for k, v in sizes.items()}
+    case["layers"] = _spread(rng, 1, share if kind == "shared" else min(8, share))
     return case
 
 
