@@ -14,6 +14,9 @@
  *                 (AdaKV budget sharing, Appendix A.1).
  *   ecokv_compact gather of the kept K/V rows into the compressed cache
  *                 (Sec. 3, selected subset).
+ * Before it: ecokv_prefill_rope (norms and rotary positions) and
+ * ecokv_prefill_write (the cache write); after it: ecokv_decode, or
+ * ecokv_append and ecokv_decode_shared for continuations of the prompts.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -365,6 +368,147 @@ int ecokv_decode_workspace_size(const ecokv_shape *shape, int32_t max_count, siz
 int ecokv_decode(const void *Q_dec, const void *Kc, const void *Vc, int dtype, const ecokv_shape *shape,
                  const int32_t *counts, const int32_t *offsets, int32_t max_count, float *O, float *lse,
                  void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- From projections to the pass, and from the compressed cache on ----
+ *
+ * The pass reads keys and window queries as attention does: normed, if the
+ * model norms them, and rotated by their positions (Sec. 3 takes Q and K as the
+ * attention's inputs).  ecokv_prefill_rope makes them from what the projections
+ * wrote; ecokv_append does the same for the tokens that continue a compressed
+ * prompt and puts their rows into a paged cache beside it; ecokv_decode_shared
+ * attends over both.  Evicted keys leave gaps in the cache but none in the
+ * positions: a continuation's first token has the position after the whole
+ * prompt's last. */
+
+/* Norm and rotary position of the rows x [D] of a token at position p:
+ *   x is scaled to x / sqrt(mean(x^2) + norm_eps) * w (w = q_norm or k_norm
+ *   [D]; NULL: not scaled);
+ *   then every pair (a, b) of rotated dimensions, pair i < rot_dim / 2, turns by
+ *   the angle p freq[i]:
+ *     a' = factor (a cos - b sin),  b' = factor (b cos + a sin);
+ *   dimensions rot_dim .. D-1 stay.
+ * Pair i is (i, i + rot_dim / 2), or (2 i, 2 i + 1) if interleaved.  Norms,
+ * angles (p freq[i] and its reduction in 64 bits) and turns are computed in
+ * 32 bits or more and rounded to the element type once, at the end. */
+typedef struct ecokv_rope {
+    int32_t rot_dim;      /* dimensions rotated: a multiple of 16 in [0, D]        */
+    int32_t interleaved;  /* 0 or 1                                               */
+    const float *freq;    /* DEVICE [rot_dim / 2], radians per position; may be   */
+                          /* NULL if rot_dim is 0 (see ecokv_rope_freqs)          */
+    float factor;         /* of cosines and sines; 1 for unscaled rotary positions */
+    float norm_eps;       /* >= 0                                                 */
+    const void *q_norm;   /* DEVICE [D] weights of the element type, or NULL      */
+    const void *k_norm;
+} ecokv_rope;
+
+/* How ecokv_rope_freqs changes the frequencies base^(-2i/rot_dim) for contexts
+ * `stretch` times as long as the model's. */
+#define ECOKV_ROPE_PLAIN 0    /* not at all (stretch is not read)                 */
+#define ECOKV_ROPE_LINEAR 1   /* all divided by stretch                           */
+#define ECOKV_ROPE_BASE 2     /* base times stretch^(rot_dim / (rot_dim - 2))     */
+#define ECOKV_ROPE_BY_PARTS 3 /* pairs that turn at least 32 times within         */
+                              /* `context` positions as they are, those that turn */
+                              /* at most once divided by stretch, a linear ramp   */
+                              /* over the turns between; factor 0.1 ln stretch + 1 */
+
+/* Host only: the frequencies of rot_dim / 2 pairs into freq (HOST) and the
+ * factor of cosines and sines into *factor (1 but for BY_PARTS).  ECOKV_EINVAL
+ * unless rot_dim is a positive even number (BASE: at least 4), base > 1,
+ * stretch >= 1, context > 0 (BY_PARTS), all finite. */
+int ecokv_rope_freqs(int rot_dim, double base, int kind, double stretch, double context, float *freq, float *factor);
+
+/* Norm and rotary positions of a prompt's queries and keys (one pass):
+ *   Q, K       DEVICE [L][T_total] rows of q_stride / k_stride elements, each
+ *              beginning with a token's [H_q][D] / [H_kv][D] elements of type
+ *              `dtype`: what a projection wrote, alone or fused with others
+ *   shape      sequences of at least one token; `window` is read only with Q_win
+ *              and may then be as long as a sequence
+ *   positions  DEVICE [T_total], or NULL: the place in the own sequence
+ *   Q_out      DEVICE [L][T_total][H_q][D], or NULL
+ *   K_out      DEVICE [L][T_total][H_kv][D], the K_new of ecokv_prefill_write
+ *   Q_win      DEVICE [L][H_q][B][w][D], the window queries that
+ *              ecokv_prefill_write and ecokv_score read, or NULL.  Without
+ *              Q_out only the window's queries are read.
+ * K and K_out are both NULL or neither; Q is NULL exactly if Q_out and Q_win
+ * are.  An output may be the input itself where that is packed (stride
+ * H D); otherwise outputs overlap neither the inputs nor each other.  Row
+ * buffers must be 16-byte aligned and strides multiples of 16 bytes of at
+ * least a token's elements.  Errors: ECOKV_EINVAL, ECOKV_EUNSUPPORTED
+ * (head_dim, dtype, rot_dim not a multiple of 16); nothing is enqueued then. */
+int ecokv_prefill_rope(const void *Q, int64_t q_stride, const void *K, int64_t k_stride, int dtype,
+                       const ecokv_shape *shape, const ecokv_rope *rope, const int32_t *positions, void *Q_out,
+                       void *K_out, void *Q_win, void *stream);
+
+/* The paged rows that continue compressed prompts.  Row r of continuation c
+ * lies in page table[c][r / page_size], at r % page_size, for every layer and
+ * KV head.  A page that two continuations share is one that both may read (the
+ * common rows of a fork, say); what is appended to it both see. */
+typedef struct ecokv_tails {
+    void *K, *V;           /* DEVICE [L][num_pages][H_kv][page_size][D]           */
+    const int32_t *table;  /* DEVICE [num_conts][max_pages]                       */
+    int32_t num_conts;     /* N                                                   */
+    int32_t num_pages;     /* >= 1                                                */
+    int32_t page_size;     /* a power of two, at most 65536                       */
+    int32_t max_pages;     /* >= 1; max_pages * page_size < 2^31                  */
+} ecokv_tails;
+
+/* New tokens of continuations: their queries and keys normed and rotated, their
+ * keys and values written to the tails.
+ *   Q_new, K_new, V_new  DEVICE [L][num_tokens] rows of q_/k_/v_stride elements,
+ *              as Q and K of ecokv_prefill_rope (V_new: [H_kv][D] elements).
+ *              Q_new may be NULL (then Q_dec too).
+ *   shape      only num_layers, num_q_heads, num_kv_heads and head_dim are read
+ *   positions  DEVICE [num_tokens]
+ *   conts      DEVICE [num_tokens] continuation of each token, or NULL: token t
+ *              continues t (num_tokens <= N)
+ *   rows       DEVICE [num_tokens] row of each token in its tail
+ *   Q_dec      DEVICE [L][H_q][num_tokens][D], the queries ecokv_decode_shared
+ *              reads where every continuation has one token, in order
+ * A token whose row is negative or past max_pages * page_size, whose
+ * continuation is not in [0, N) or whose page is not in [0, num_pages) is not
+ * written to the tails (its query is); so a padded batch marks its padding with
+ * rows of -1.  Two tokens of a call must not have one row: what it holds then
+ * is not defined.  The tails and Q_dec overlap neither each other nor the new
+ * rows.  Alignment and errors as ecokv_prefill_rope. */
+int ecokv_append(const void *Q_new, int64_t q_stride, const void *K_new, int64_t k_stride, const void *V_new,
+                 int64_t v_stride, int dtype, const ecokv_shape *shape, const ecokv_rope *rope,
+                 const int32_t *positions, const int32_t *conts, const int32_t *rows, int32_t num_tokens,
+                 const ecokv_tails *tails, void *Q_dec, void *stream);
+
+/* Workspace bytes of ecokv_decode_shared for this shape, fan and these bounds. */
+int ecokv_decode_shared_workspace_size(const ecokv_shape *shape, const int32_t *fan, int32_t max_count,
+                                       int32_t max_tail, size_t *bytes);
+
+/* Decode attention of a batch whose sequences share compressed prompts: one
+ * query of each of N continuations over its prompt's kept rows, which all
+ * continuations of the prompt read at once, and its own tail.
+ *   shape   of the prompts (the B sequences of the pass)
+ *   fan     HOST [B + 1], nondecreasing from 0: prompt s is continued by
+ *           continuations fan[s] .. fan[s + 1] - 1 (perhaps none); N = fan[B]
+ *   Q_dec   DEVICE [L][H_q][N][D] (dtype), rotated
+ *   Kc, Vc, counts, offsets, max_count
+ *           the compressed cache, as for ecokv_decode; max_count may be 0 (no
+ *           prompt rows: Kc, Vc, counts and offsets are not read and may be NULL)
+ *   tails   the paged rows (their K and V of type dtype), tails->num_conts = N;
+ *           may be NULL if max_tail is 0 (then tail_counts too)
+ *   tail_counts  DEVICE [N]: rows 0 .. tail_counts[c] - 1 of continuation c's
+ *           tail are attended, for every layer
+ *   max_tail  an upper bound of every tail_counts[c], at most
+ *           max_pages * page_size
+ *   O       DEVICE [L][H_q][N][D] float32;  lse [L][H_q][N] float32 or NULL:
+ *             O = sum_j softmax_j(q . k_j / sqrt(D)) v_j,
+ *             lse = log sum_j exp(q . k_j / sqrt(D)),
+ *           j over both sets of rows; O 0 and lse -inf where there are none.
+ * A count below 0 or above its bound, and a page outside [0, num_pages) among
+ * the attended rows, give NaN outputs for the continuations concerned.
+ * Arithmetic: fp32 accumulation (bf16 rows: the weights as three bf16 summands
+ * each, 24 bits, so a value row with an infinity gives NaN).
+ * Q_dec, Kc, Vc and the tails' K and V must be 16-byte aligned, the workspace
+ * 256-byte aligned; it needs no initial contents. */
+int ecokv_decode_shared(const void *Q_dec, const void *Kc, const void *Vc, int dtype, const ecokv_shape *shape,
+                        const int32_t *fan, const int32_t *counts, const int32_t *offsets, int32_t max_count,
+                        const ecokv_tails *tails, const int32_t *tail_counts, int32_t max_tail, float *O, float *lse,
+                        void *workspace, size_t workspace_bytes, void *stream);
 
 /* PyramidKV's layer schedule (Appendix A.1), host only: for m = num_layers
  * layers sharing `total` tokens per head, the last layer gets

@@ -30,7 +30,8 @@ struct ShapeInfo {
     int maxT, maxP;
 };
 
-int check_shape(const ecokv_shape *sh, ShapeInfo *o)
+// The layers, heads and head_dim of a shape.
+int check_heads(const ecokv_shape *sh, ShapeInfo *o)
 {
     if (!sh) return fail(ECOKV_EINVAL, "shape is NULL");
     if (sh->num_layers < 0) return fail(ECOKV_EINVAL, "num_layers %d < 0", sh->num_layers);
@@ -40,7 +41,17 @@ int check_shape(const ecokv_shape *sh, ShapeInfo *o)
                     sh->num_kv_heads);
     if (sh->head_dim != 64 && sh->head_dim != 128)
         return fail(ECOKV_EUNSUPPORTED, "head_dim %d (supported: 64, 128)", sh->head_dim);
-    if (sh->window < 1) return fail(ECOKV_EINVAL, "window %d < 1", sh->window);
+    o->L = sh->num_layers;
+    o->Hq = sh->num_q_heads;
+    o->Hkv = sh->num_kv_heads;
+    o->G = o->Hq / o->Hkv;
+    o->D = sh->head_dim;
+    return ECOKV_OK;
+}
+
+// And its sequences, of more than `shortest` tokens.
+int check_seqs(const ecokv_shape *sh, int shortest, ShapeInfo *o)
+{
     if (sh->num_seqs < 1 || sh->num_seqs > ECOKV_MAX_SEQS)
         return fail(ECOKV_EINVAL, "num_seqs %d outside [1, %d]", sh->num_seqs, ECOKV_MAX_SEQS);
     if (!sh->cu_seqlens) return fail(ECOKV_EINVAL, "cu_seqlens is NULL");
@@ -48,20 +59,25 @@ int check_shape(const ecokv_shape *sh, ShapeInfo *o)
     o->maxT = 0;
     for (int s = 0; s < sh->num_seqs; ++s) {
         const int64_t T = (int64_t)sh->cu_seqlens[s + 1] - sh->cu_seqlens[s];
-        if (T <= sh->window)
+        if (T <= shortest && shortest > 0)
             return fail(ECOKV_EINVAL, "sequence %d has %lld tokens; the window %d must be shorter", s, (long long)T,
-                        sh->window);
+                        shortest);
+        if (T <= shortest) return fail(ECOKV_EINVAL, "sequence %d has %lld tokens", s, (long long)T);
         if (T > o->maxT) o->maxT = (int)T;
     }
-    o->L = sh->num_layers;
-    o->Hq = sh->num_q_heads;
-    o->Hkv = sh->num_kv_heads;
-    o->G = o->Hq / o->Hkv;
-    o->D = sh->head_dim;
-    o->w = sh->window;
     o->B = sh->num_seqs;
-    o->R = o->G * o->w;
     o->Ttot = sh->cu_seqlens[o->B];
+    return ECOKV_OK;
+}
+
+int check_shape(const ecokv_shape *sh, ShapeInfo *o)
+{
+    int rc = check_heads(sh, o);
+    if (rc) return rc;
+    if (sh->window < 1) return fail(ECOKV_EINVAL, "window %d < 1", sh->window);
+    if ((rc = check_seqs(sh, sh->window, o))) return rc;
+    o->w = sh->window;
+    o->R = o->G * o->w;
     o->Ptot = o->Ttot - (int64_t)o->B * o->w;
     o->maxP = o->maxT - o->w;
     if ((int64_t)o->L * o->Hkv * o->B > (int64_t)INT32_MAX / 8)
@@ -811,6 +827,310 @@ int ecokv_decode(const void *Q_dec, const void *Kc, const void *Vc, int dtype, c
     const hipError_t e = ecokv::decode_launch(a, static_cast<char *>(workspace), workspace_bytes, dtype == ECOKV_BF16,
                                              static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "ecokv_decode launch");
+    return ECOKV_OK;
+}
+
+int ecokv_rope_freqs(int rot_dim, double base, int kind, double stretch, double context, float *freq, float *factor)
+{
+    if (rot_dim < 2 || rot_dim % 2 != 0 || !freq || !factor)
+        return fail(ECOKV_EINVAL, "rot_dim %d is not a positive even number, or freq or factor is NULL", rot_dim);
+    if (kind < ECOKV_ROPE_PLAIN || kind > ECOKV_ROPE_BY_PARTS) return fail(ECOKV_EINVAL, "kind %d", kind);
+    if (!(isfinite(base) && base > 1.0)) return fail(ECOKV_EINVAL, "base %g", base);
+    if (kind != ECOKV_ROPE_PLAIN && !(isfinite(stretch) && stretch >= 1.0)) return fail(ECOKV_EINVAL, "stretch %g", stretch);
+    if (kind == ECOKV_ROPE_BASE && rot_dim < 4) return fail(ECOKV_EINVAL, "rot_dim %d with a stretched base", rot_dim);
+    if (kind == ECOKV_ROPE_BY_PARTS && !(isfinite(context) && context > 0.0)) return fail(ECOKV_EINVAL, "context %g", context);
+    if (kind == ECOKV_ROPE_BASE) base *= pow(stretch, (double)rot_dim / (rot_dim - 2));
+    if (!isfinite(base)) return fail(ECOKV_EINVAL, "the stretched base is not finite");
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        double f = pow(base, -2.0 * i / rot_dim);
+        if (kind == ECOKV_ROPE_LINEAR) f /= stretch;
+        if (kind == ECOKV_ROPE_BY_PARTS) {
+            const double turns = context * f / 6.283185307179586477;
+            const double keep = fmin(fmax((turns - 1.0) / 31.0, 0.0), 1.0);  // 1 turn .. 32 turns
+            f *= keep + (1.0 - keep) / stretch;
+        }
+        freq[i] = (float)f;
+    }
+    *factor = kind == ECOKV_ROPE_BY_PARTS ? (float)(0.1 * log(stretch) + 1.0) : 1.f;
+    return ECOKV_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// Bytes [p, p + n) of an argument, and whether two share any.
+struct Span {
+    const void *p;
+    size_t n;
+};
+bool overlap(const Span &x, const Span &y)
+{
+    const uintptr_t a = (uintptr_t)x.p, b = (uintptr_t)y.p;
+    return x.p && y.p && x.n && y.n && a < b + y.n && b < a + x.n;
+}
+
+int check_rope(const ecokv_rope *r, int D)
+{
+    if (!r) return fail(ECOKV_EINVAL, "rope is NULL");
+    if (r->rot_dim < 0 || r->rot_dim > D || r->rot_dim % 2 != 0)
+        return fail(ECOKV_EINVAL, "rot_dim %d is not an even number in [0, %d]", r->rot_dim, D);
+    if (r->rot_dim % 16 != 0) return fail(ECOKV_EUNSUPPORTED, "rot_dim %d (supported: multiples of 16)", r->rot_dim);
+    if (r->interleaved != 0 && r->interleaved != 1) return fail(ECOKV_EINVAL, "interleaved must be 0 or 1");
+    if (r->rot_dim > 0 && !r->freq) return fail(ECOKV_EINVAL, "freq is NULL");
+    if (!isfinite(r->factor)) return fail(ECOKV_EINVAL, "factor %g", (double)r->factor);
+    if (!(isfinite(r->norm_eps) && r->norm_eps >= 0.f)) return fail(ECOKV_EINVAL, "norm_eps %g", (double)r->norm_eps);
+    return ECOKV_OK;
+}
+
+// Rows of `tokens` tokens with `elems` elements of size es each, `stride`
+// elements from token to token.
+int check_rows(const void *p, int64_t stride, int64_t tokens, int64_t elems, int es, const char *name, Span *span)
+{
+    if (((uintptr_t)p & 15u) != 0) return fail(ECOKV_EINVAL, "%s must be 16-byte aligned", name);
+    if (stride < elems || stride * es % 16 != 0 || stride > INT64_MAX / 4 / (tokens > 0 ? tokens : 1) / es)
+        return fail(ECOKV_EINVAL, "the stride %lld of %s is below a token's %lld elements or no multiple of 16 bytes",
+                    (long long)stride, name, (long long)elems);
+    *span = Span{p, tokens > 0 ? (size_t)((tokens - 1) * stride + elems) * es : 0};
+    return ECOKV_OK;
+}
+
+int check_tails(const ecokv_tails *t, const ShapeInfo &si, int es, ecokv::TailMap *m, Span *K, Span *V)
+{
+    if (!t) return fail(ECOKV_EINVAL, "tails is NULL");
+    if (t->num_conts < 0 || t->num_pages < 1 || t->max_pages < 1)
+        return fail(ECOKV_EINVAL, "tails: num_conts %d, num_pages %d, max_pages %d", t->num_conts, t->num_pages, t->max_pages);
+    if (t->page_size < 1 || t->page_size > 65536 || (t->page_size & (t->page_size - 1)) != 0)
+        return fail(ECOKV_EINVAL, "page_size %d is not a power of two of at most 65536", t->page_size);
+    if ((int64_t)t->max_pages * t->page_size > INT32_MAX) return fail(ECOKV_EINVAL, "a tail of 2^31 rows or more");
+    if (!t->K || !t->V || !t->table) return fail(ECOKV_EINVAL, "the tails' K, V and table must be non-NULL");
+    if ((((uintptr_t)t->K | (uintptr_t)t->V) & 15u) != 0)
+        return fail(ECOKV_EINVAL, "the tails' K and V must be 16-byte aligned");
+    int shift = 0;
+    while ((1 << shift) < t->page_size) ++shift;
+    *m = ecokv::TailMap{t->table, t->num_conts, t->num_pages, shift, t->max_pages};
+    const size_t n = (size_t)si.L * t->num_pages * si.Hkv * (size_t)t->page_size * si.D * es;
+    *K = Span{t->K, n};
+    *V = Span{t->V, n};
+    return ECOKV_OK;
+}
+
+void fill_rope(const ecokv_rope *r, ecokv::RopeArgs *a)
+{
+    a->rot = r->rot_dim;
+    a->interleaved = r->interleaved;
+    a->freq = r->freq;
+    a->factor = r->factor;
+    a->eps = r->norm_eps;
+    a->qw = r->q_norm;
+    a->kw = r->k_norm;
+}
+
+int check_fan(const ShapeInfo &si, const int32_t *fan)
+{
+    if (!fan) return fail(ECOKV_EINVAL, "fan is NULL");
+    if (fan[0] != 0) return fail(ECOKV_EINVAL, "fan[0] = %d, must be 0", fan[0]);
+    for (int s = 0; s < si.B; ++s)
+        if (fan[s + 1] < fan[s]) return fail(ECOKV_EINVAL, "fan[%d] = %d is below fan[%d] = %d", s + 1, fan[s + 1], s, fan[s]);
+    if ((int64_t)(si.L > 0 ? si.L : 1) * si.Hq > (int64_t)INT32_MAX / (fan[si.B] > 0 ? fan[si.B] : 1))
+        return fail(ECOKV_EINVAL, "too many (layer, query head, continuation) rows");
+    return ECOKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ecokv_prefill_rope(const void *Q, int64_t q_stride, const void *K, int64_t k_stride, int dtype,
+                       const ecokv_shape *shape, const ecokv_rope *rope, const int32_t *positions, void *Q_out,
+                       void *K_out, void *Q_win, void *stream)
+{
+    ShapeInfo si;
+    memset(&si, 0, sizeof si);
+    int rc = check_heads(shape, &si);
+    if (rc) return rc;
+    if ((rc = check_seqs(shape, 0, &si))) return rc;
+    if (dtype != ECOKV_BF16 && dtype != ECOKV_F32) return fail(ECOKV_EUNSUPPORTED, "dtype %d", dtype);
+    if ((rc = check_rope(rope, si.D))) return rc;
+    if (Q_win)
+        for (int s = 0; s < si.B; ++s)
+            if (shape->window < 1 || shape->cu_seqlens[s + 1] - shape->cu_seqlens[s] < shape->window)
+                return fail(ECOKV_EINVAL, "window %d is below 1 or longer than sequence %d", shape->window, s);
+    if (si.L == 0) return ECOKV_OK;
+    if ((K == nullptr) != (K_out == nullptr)) return fail(ECOKV_EINVAL, "K and K_out: both or neither");
+    if ((Q == nullptr) != (Q_out == nullptr && Q_win == nullptr))
+        return fail(ECOKV_EINVAL, "Q goes with Q_out, Q_win or both");
+    const int es = dtype == ECOKV_BF16 ? 2 : 4;
+    const int64_t tokens = (int64_t)si.L * si.Ttot, qe = (int64_t)si.Hq * si.D, ke = (int64_t)si.Hkv * si.D;
+    Span q{}, k{};
+    if (Q && (rc = check_rows(Q, q_stride, tokens, qe, es, "Q", &q))) return rc;
+    if (K && (rc = check_rows(K, k_stride, tokens, ke, es, "K", &k))) return rc;
+    const Span qo{Q_out, (size_t)(tokens * qe * es)}, ko{K_out, (size_t)(tokens * ke * es)},
+        qw{Q_win, (size_t)(qe * si.L * si.B * (Q_win ? shape->window : 0) * es)};
+    if ((((uintptr_t)Q_out | (uintptr_t)K_out | (uintptr_t)Q_win) & 15u) != 0)
+        return fail(ECOKV_EINVAL, "Q_out, K_out and Q_win must be 16-byte aligned");
+    // in place: a packed input onto itself
+    const bool qi = Q && Q_out == Q && q_stride == qe, ki = K && K_out == K && k_stride == ke;
+    if ((!qi && overlap(qo, q)) || (!ki && overlap(ko, k)) || overlap(qo, k) || overlap(ko, q) || overlap(qw, q) ||
+        overlap(qw, k) || overlap(qo, ko) || overlap(qo, qw) || overlap(ko, qw))
+        return fail(ECOKV_EINVAL, "an output overlaps an input or another output");
+    if (!Q && !K) return ECOKV_OK;
+    ecokv::RopeArgs a;
+    memset(&a, 0, sizeof a);
+    a.Q = static_cast<const char *>(Q);
+    a.K = static_cast<const char *>(K);
+    a.Qo = static_cast<char *>(Q_out);
+    a.Ko = static_cast<char *>(K_out);
+    a.win = static_cast<char *>(Q_win);
+    a.q_stride = q_stride * es;
+    a.k_stride = k_stride * es;
+    a.positions = positions;
+    fill_rope(rope, &a);
+    a.L = si.L;
+    a.n = (int)si.Ttot;
+    a.Hq = si.Hq;
+    a.Hkv = si.Hkv;
+    a.B = si.B;
+    a.w = shape->window;
+    a.hq = Q ? si.Hq : 0;
+    a.hk = K ? si.Hkv : 0;
+    if ((rc = fill_seqtab(shape, nullptr, 0, &a.seq, nullptr))) return rc;
+    const hipError_t e = ecokv::rope_launch(a, false, dtype == ECOKV_BF16, si.D, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "ecokv_prefill_rope launch");
+    return ECOKV_OK;
+}
+
+int ecokv_append(const void *Q_new, int64_t q_stride, const void *K_new, int64_t k_stride, const void *V_new,
+                 int64_t v_stride, int dtype, const ecokv_shape *shape, const ecokv_rope *rope,
+                 const int32_t *positions, const int32_t *conts, const int32_t *rows, int32_t num_tokens,
+                 const ecokv_tails *tails, void *Q_dec, void *stream)
+{
+    ShapeInfo si;
+    memset(&si, 0, sizeof si);
+    int rc = check_heads(shape, &si);
+    if (rc) return rc;
+    if (dtype != ECOKV_BF16 && dtype != ECOKV_F32) return fail(ECOKV_EUNSUPPORTED, "dtype %d", dtype);
+    if ((rc = check_rope(rope, si.D))) return rc;
+    if (num_tokens < 0) return fail(ECOKV_EINVAL, "num_tokens %d < 0", num_tokens);
+    if (si.L == 0 || num_tokens == 0) return ECOKV_OK;
+    const int es = dtype == ECOKV_BF16 ? 2 : 4;
+    ecokv::RopeArgs a;
+    memset(&a, 0, sizeof a);
+    Span tk{}, tv{}, q{}, k{}, v{};
+    if ((rc = check_tails(tails, si, es, &a.map, &tk, &tv))) return rc;
+    if (!K_new || !V_new || !positions || !rows)
+        return fail(ECOKV_EINVAL, "K_new, V_new, positions and rows must be non-NULL");
+    if ((Q_new == nullptr) != (Q_dec == nullptr)) return fail(ECOKV_EINVAL, "Q_new and Q_dec: both or neither");
+    if (!conts && num_tokens > tails->num_conts)
+        return fail(ECOKV_EINVAL, "without conts, %d tokens need as many continuations (%d)", num_tokens, tails->num_conts);
+    const int64_t tokens = (int64_t)si.L * num_tokens, qe = (int64_t)si.Hq * si.D, ke = (int64_t)si.Hkv * si.D;
+    if (Q_new && (rc = check_rows(Q_new, q_stride, tokens, qe, es, "Q_new", &q))) return rc;
+    if ((rc = check_rows(K_new, k_stride, tokens, ke, es, "K_new", &k))) return rc;
+    if ((rc = check_rows(V_new, v_stride, tokens, ke, es, "V_new", &v))) return rc;
+    if (((uintptr_t)Q_dec & 15u) != 0) return fail(ECOKV_EINVAL, "Q_dec must be 16-byte aligned");
+    const Span out[3] = {tk, tv, Span{Q_dec, (size_t)(tokens * qe * es)}}, in[3] = {q, k, v};
+    for (int i = 0; i < 3; ++i)
+        for (int j = 0; j < 3; ++j)
+            if (overlap(out[i], in[j]) || (i < j && overlap(out[i], out[j])))
+                return fail(ECOKV_EINVAL, "the tails, Q_dec and the new rows must not overlap");
+    a.Q = static_cast<const char *>(Q_new);
+    a.K = static_cast<const char *>(K_new);
+    a.V = static_cast<const char *>(V_new);
+    a.Qo = static_cast<char *>(Q_dec);
+    a.Ko = static_cast<char *>(tails->K);
+    a.Vo = static_cast<char *>(tails->V);
+    a.q_stride = q_stride * es;
+    a.k_stride = k_stride * es;
+    a.v_stride = v_stride * es;
+    a.positions = positions;
+    a.conts = conts;
+    a.rows = rows;
+    fill_rope(rope, &a);
+    a.L = si.L;
+    a.n = num_tokens;
+    a.Hq = si.Hq;
+    a.Hkv = si.Hkv;
+    a.B = 1;
+    a.hq = Q_new ? si.Hq : 0;
+    a.hk = si.Hkv;
+    const hipError_t e = ecokv::rope_launch(a, true, dtype == ECOKV_BF16, si.D, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "ecokv_append launch");
+    return ECOKV_OK;
+}
+
+int ecokv_decode_shared_workspace_size(const ecokv_shape *shape, const int32_t *fan, int32_t max_count,
+                                       int32_t max_tail, size_t *bytes)
+{
+    ShapeInfo si;
+    int rc = check_shape(shape, &si);
+    if (rc) return rc;
+    if ((rc = check_fan(si, fan))) return rc;
+    if (!bytes) return fail(ECOKV_EINVAL, "bytes is NULL");
+    if (max_count < 0 || max_tail < 0) return fail(ECOKV_EINVAL, "max_count %d or max_tail %d < 0", max_count, max_tail);
+    *bytes = ecokv::shared_grid((int64_t)si.L * si.Hkv, si.G, si.D, si.B, fan, max_count, max_tail).bytes;
+    return ECOKV_OK;
+}
+
+int ecokv_decode_shared(const void *Q_dec, const void *Kc, const void *Vc, int dtype, const ecokv_shape *shape,
+                        const int32_t *fan, const int32_t *counts, const int32_t *offsets, int32_t max_count,
+                        const ecokv_tails *tails, const int32_t *tail_counts, int32_t max_tail, float *O, float *lse,
+                        void *workspace, size_t workspace_bytes, void *stream)
+{
+    ShapeInfo si;
+    int rc = check_shape(shape, &si);
+    if (rc) return rc;
+    if (dtype != ECOKV_BF16 && dtype != ECOKV_F32) return fail(ECOKV_EUNSUPPORTED, "dtype %d", dtype);
+    if ((rc = check_fan(si, fan))) return rc;
+    if (max_count < 0 || max_tail < 0) return fail(ECOKV_EINVAL, "max_count %d or max_tail %d < 0", max_count, max_tail);
+    if (si.L == 0 || fan[si.B] == 0) return ECOKV_OK;
+    ecokv::SharedArgs a;
+    memset(&a, 0, sizeof a);
+    if (!Q_dec || !O) return fail(ECOKV_EINVAL, "Q_dec and O must be non-NULL");
+    if (max_count > 0 && (!Kc || !Vc || !counts || !offsets))
+        return fail(ECOKV_EINVAL, "Kc, Vc, counts and offsets must be non-NULL");
+    if ((((uintptr_t)Q_dec | (uintptr_t)Kc | (uintptr_t)Vc) & 15u) != 0)
+        return fail(ECOKV_EINVAL, "Q_dec, Kc and Vc must be 16-byte aligned");
+    if (max_tail > 0) {
+        Span tk, tv;
+        if ((rc = check_tails(tails, si, dtype == ECOKV_BF16 ? 2 : 4, &a.map, &tk, &tv))) return rc;
+        if (!tail_counts) return fail(ECOKV_EINVAL, "tail_counts must be non-NULL");
+        if (tails->num_conts != fan[si.B])
+            return fail(ECOKV_EINVAL, "the tails have %d continuations, fan %d", tails->num_conts, fan[si.B]);
+        if ((int64_t)max_tail > (int64_t)tails->max_pages * tails->page_size)
+            return fail(ECOKV_EINVAL, "max_tail %d is more rows than %d pages of %d hold", max_tail, tails->max_pages,
+                        tails->page_size);
+    }
+    a.grid = ecokv::shared_grid((int64_t)si.L * si.Hkv, si.G, si.D, si.B, fan, max_count, max_tail);
+    if (!workspace) return fail(ECOKV_EINVAL, "workspace is NULL");
+    if (((uintptr_t)workspace & 255u) != 0) return fail(ECOKV_EINVAL, "workspace must be 256-byte aligned");
+    if (workspace_bytes < a.grid.bytes)
+        return fail(ECOKV_EWORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, a.grid.bytes);
+    a.Q = static_cast<const char *>(Q_dec);
+    a.Kc = static_cast<const char *>(Kc);
+    a.Vc = static_cast<const char *>(Vc);
+    a.Kt = max_tail > 0 ? static_cast<const char *>(tails->K) : nullptr;
+    a.Vt = max_tail > 0 ? static_cast<const char *>(tails->V) : nullptr;
+    a.counts = counts;
+    a.offsets = offsets;
+    a.tail_counts = tail_counts;
+    a.O = O;
+    a.lse = lse;
+    // (the sums first: they stay 16-byte aligned)
+    a.acc = static_cast<float *>(workspace);
+    a.ms = reinterpret_cast<float2 *>(a.acc + (size_t)(a.grid.np + a.grid.nt) * (size_t)a.grid.qrows * si.D);
+    a.L = si.L;
+    a.Hq = si.Hq;
+    a.Hkv = si.Hkv;
+    a.G = si.G;
+    a.B = si.B;
+    a.N = fan[si.B];
+    a.D = si.D;
+    a.max_count = max_count;
+    a.max_tail = max_tail;
+    a.qscale = 1.4426950408889634f / sqrtf((float)si.D);
+    for (int s = 0; s <= si.B; ++s) a.fan[s] = fan[s];
+    const hipError_t e = ecokv::shared_launch(a, dtype == ECOKV_BF16, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "ecokv_decode_shared launch");
     return ECOKV_OK;
 }
 

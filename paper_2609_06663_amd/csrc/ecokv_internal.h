@@ -6,6 +6,7 @@
 
 #include "ecokv.h"
 #include "ecokv_decode_plan.h"
+#include "ecokv_shared_plan.h"
 
 namespace ecokv {
 
@@ -218,6 +219,42 @@ struct DecodeArgs {
 size_t decode_ws_bytes(int64_t units, int G, int D, int max_count, bool least);
 // Plans within ws_bytes (at least the least) and launches the decode and merge kernels.
 hipError_t decode_launch(DecodeArgs a, char *ws, size_t ws_bytes, bool bf16, hipStream_t st);
+
+// Norms and rotary positions of a prompt's tokens, or of tokens appended to
+// the tails.  Strides in bytes from token to token.
+struct RopeArgs {
+    const char *Q, *K, *V;
+    char *Qo, *Ko, *Vo;   // prefill: [L][n][Hq][D], [L][n][Hkv][D]; append: Q_dec [L][Hq][n][D], the tails' K and V
+    char *win;            // [L][Hq][B][w][D] or null
+    int64_t q_stride, k_stride, v_stride;
+    const int32_t *positions, *conts, *rows;
+    const float *freq;
+    const void *qw, *kw;
+    float factor, eps;
+    int rot, interleaved;
+    int L, n, Hq, Hkv, B, w;
+    int hq, hk;           // query and KV heads that the call handles (0: none)
+    int per_block;        // tokens per block
+    TailMap map;
+    SeqTab seq;
+};
+hipError_t rope_launch(RopeArgs a, bool append, bool bf16, int D, hipStream_t st);
+
+// Decode attention of continuations over shared prompts and paged tails.
+struct SharedArgs {
+    const char *Q, *Kc, *Vc, *Kt, *Vt;
+    const int32_t *counts, *offsets, *tail_counts;
+    float *O, *lse;
+    float *acc;           // [np + nt][L Hq N][D] partial sums
+    float2 *ms;           // [np + nt][L Hq N] their (maximum, sum)
+    int L, Hq, Hkv, G, B, N, D;
+    int max_count, max_tail;
+    float qscale;         // log2(e) / sqrt(D)
+    TailMap map;
+    SharedGrid grid;
+    int fan[ECOKV_MAX_SEQS + 1];
+};
+hipError_t shared_launch(SharedArgs a, bool bf16, hipStream_t st);
 
 // The sweeps of ecokv_sweep.hip (every dtype, head_dim and number of window
 // rows): pass 1 or 2 over blocks of a.rpb1 / a.rpb2 keys, a multiple of 128

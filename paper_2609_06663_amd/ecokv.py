@@ -26,6 +26,7 @@ IMP_ATTN, IMP_ATTN_VNORM = 0, 1
 NORM_MINMAX, NORM_WINSOR, NORM_MAD = 0, 1, 2
 RED_EUCLID, RED_STD = 0, 1
 CENTROID_ALL, CENTROID_PREFIX = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = 0, 1, 2, 3
 MAX_SEQS, MAX_ROWS = 64, 64
 NSTATS = 12
 STAT = dict(lambda_=0, rC=1, rE=2, DE=3, dmin=4, dmax=5, sdmin=6, sdmax=7, imp_mean=8, sbar_mean=9,
@@ -37,6 +38,8 @@ EXPORTS = ["ecokv_default_params", "ecokv_workspace_size", "ecokv_workspace_stat
            "ecokv_index_count_mode", "ecokv_select_workspace_size", "ecokv_select", "ecokv_compact",
            "ecokv_pyramid_budgets",
            "ecokv_decode_workspace_size", "ecokv_decode",
+           "ecokv_rope_freqs", "ecokv_prefill_rope", "ecokv_append", "ecokv_decode_shared_workspace_size",
+           "ecokv_decode_shared",
            "ecokv_last_error", "ecokv_stage_times"]
 
 
@@ -111,6 +114,61 @@ class Shape:
         return self.c.num_layers * self.c.num_kv_heads * self.ptot
 
 
+class _Rope(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("freq", ctypes.c_void_p),
+                ("factor", ctypes.c_float), ("norm_eps", ctypes.c_float), ("q_norm", ctypes.c_void_p),
+                ("k_norm", ctypes.c_void_p)]
+
+
+class Rope:
+    """ecokv_rope: rotary positions (`freq` float32 [rot_dim / 2], see
+    ecokv_rope_freqs) and, where `q_norm` / `k_norm` [D] weights are given, the
+    per-head norms before them.  Holds the tensors that it points to."""
+
+    def __init__(self, rot_dim: int, freq: Optional[torch.Tensor] = None, interleaved: bool = False, factor: float = 1.0,
+                 q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, norm_eps: float = 1e-6):
+        self.freq, self.q_norm, self.k_norm = freq, q_norm, k_norm
+        self.c = _Rope(int(rot_dim), int(bool(interleaved)), None, factor, norm_eps, None, None)
+
+    def _arg(self, head_dim: int, dtype, device):
+        """Pointer to the checked structure, for rows of this element type."""
+        self.c.freq = _arg(self.freq, "freq", _F32, max(self.c.rot_dim, 0) // 2, device, optional=self.c.rot_dim <= 0)
+        self.c.q_norm = _arg(self.q_norm, "q_norm", (dtype,), head_dim, device, optional=True)
+        self.c.k_norm = _arg(self.k_norm, "k_norm", (dtype,), head_dim, device, optional=True)
+        return ctypes.byref(self.c)
+
+
+class _Tails(ctypes.Structure):
+    _fields_ = [("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("num_conts", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32)]
+
+
+class Tails:
+    """ecokv_tails: K, V [L][num_pages][H_kv][page_size][D] and table (int32)
+    [num_conts][max_pages].  Holds the tensors that it points to."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor):
+        if K.dim() != 5 or V.shape != K.shape or V.dtype != K.dtype:
+            raise ValueError("the tails' K and V are two tensors [L][num_pages][H_kv][page_size][D] of one element type")
+        if table.dim() != 2:
+            raise ValueError("the tails' table is [num_conts][max_pages]")
+        self.K, self.V, self.table = K, V, table
+        self.c = _Tails(None, None, None, table.shape[0], K.shape[1], K.shape[3], table.shape[1])
+
+    def _arg(self, shape: "Shape", dtype, device):
+        """Pointer to the checked structure, for calls of this shape and element type."""
+        c = shape.c
+        L, _, H, _, D = self.K.shape
+        if (L, H, D) != (c.num_layers, c.num_kv_heads, c.head_dim):
+            raise ValueError(f"the tails have {L} layers of {H} KV heads of {D} dimensions, the shape "
+                             f"{c.num_layers} of {c.num_kv_heads} of {c.head_dim}")
+        self.c.K = _arg(self.K, "the tails' K", (dtype,), self.K.numel(), device)
+        self.c.V = _arg(self.V, "the tails' V", (dtype,), self.K.numel(), device)
+        self.c.table = _arg(self.table, "the tails' table", _I32, self.table.numel(), device)
+        return ctypes.byref(self.c)
+
+
 def _load():
     if not os.path.exists(_LIB_PATH):
         raise ImportError(f"{_LIB_PATH} is not built; run `python paper_2609_06663_amd/build.py`")
@@ -131,6 +189,16 @@ def _load():
     lib.ecokv_decode_workspace_size.argtypes = [sp, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
     lib.ecokv_decode.argtypes = [vp, vp, vp, ctypes.c_int, sp, vp, vp, ctypes.c_int32, vp, vp, vp,
                                  ctypes.c_size_t, vp]
+    rp, tp, i64 = ctypes.POINTER(_Rope), ctypes.POINTER(_Tails), ctypes.c_int64
+    f32p = ctypes.POINTER(ctypes.c_float)
+    lib.ecokv_rope_freqs.argtypes = [ctypes.c_int, ctypes.c_double, ctypes.c_int, ctypes.c_double, ctypes.c_double,
+                                     f32p, f32p]
+    lib.ecokv_prefill_rope.argtypes = [vp, i64, vp, i64, ctypes.c_int, sp, rp, vp, vp, vp, vp, vp]
+    lib.ecokv_append.argtypes = [vp, i64, vp, i64, vp, i64, ctypes.c_int, sp, rp, vp, vp, vp, ctypes.c_int32, tp, vp, vp]
+    lib.ecokv_decode_shared_workspace_size.argtypes = [sp, i32p, ctypes.c_int32, ctypes.c_int32,
+                                                       ctypes.POINTER(ctypes.c_size_t)]
+    lib.ecokv_decode_shared.argtypes = [vp, vp, vp, ctypes.c_int, sp, i32p, vp, vp, ctypes.c_int32, tp, vp,
+                                        ctypes.c_int32, vp, vp, vp, ctypes.c_size_t, vp]
     lib.ecokv_pyramid_budgets.argtypes = [ctypes.c_int, ctypes.c_double, ctypes.c_double, ctypes.c_int, i32p]
     lib.ecokv_select_workspace_size.argtypes = [sp, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]
     lib.ecokv_select.argtypes = [vp, sp, ctypes.c_int, i32p, vp, vp, vp, vp, ctypes.c_size_t, vp]
@@ -500,6 +568,162 @@ def ecokv_decode(Q_dec: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, shape:
                             _arg(offsets, "offsets", _I32, shape.units, dev), int(max_count),
                             _arg(O, "O", _F32, nq * D, dev), _arg(lse, "lse", _F32, nq, dev, optional=True),
                             _arg(workspace, "workspace", _U8, need, dev), workspace.numel(), _stream(stream)))
+
+
+def _enqueue(fn, device, stream, *args):
+    """fn(*args, stream) on `stream` or the current stream of the tensors' device."""
+    if stream is not None and stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the call's tensors on {device}")
+    if device.index == torch._C._cuda_getDevice():
+        _check(fn(*args, _stream(stream)))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream(stream)))
+
+
+def _token_rows(t: Optional[torch.Tensor], name: str, dtype, layers: int, tokens: int, heads: int, dim: int, device):
+    """(pointer, stride) of rows [L][tokens][heads][dim] (or, for one layer,
+    [tokens][heads][dim]) that may lie further apart than they are long: a view
+    of a fused projection's output, say."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor (got {t.device})")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the call's tensors on {device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {_ELEM.get(dtype, str(dtype))} (got {t.dtype})")
+    want = (layers, tokens, heads, dim)
+    if tuple(t.shape) != want and not (layers == 1 and tuple(t.shape) == want[1:]):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, the call needs {want}")
+    packed = heads * dim
+    s = t.stride()
+    stride = s[-3] if tokens > 1 else s[0] if layers > 1 else packed
+    if t.numel() and ((dim > 1 and s[-1] != 1) or (heads > 1 and s[-2] != dim)
+                      or (layers > 1 and s[0] != tokens * stride)):
+        raise ValueError(f"{name}: the heads of a token must lie together and the tokens of all layers evenly apart")
+    return t.data_ptr(), max(stride, packed) if not t.numel() else stride
+
+
+def ecokv_rope_freqs(rot_dim: int, base: float = 10000.0, kind: int = ROPE_PLAIN, stretch: float = 1.0,
+                     context: float = 0.0):
+    """(frequencies as a list of rot_dim / 2 floats, factor) for Rope: radians per position of each pair."""
+    out = (ctypes.c_float * max(int(rot_dim) // 2, 1))()
+    factor = ctypes.c_float(0.0)
+    _check(lib.ecokv_rope_freqs(int(rot_dim), float(base), int(kind), float(stretch), float(context), out,
+                                ctypes.byref(factor)))
+    return [float(v) for v in out], float(factor.value)
+
+
+def ecokv_prefill_rope(Q: Optional[torch.Tensor], K: Optional[torch.Tensor], shape: Shape, rope: Rope,
+                       positions: Optional[torch.Tensor] = None, Q_out: Optional[torch.Tensor] = None,
+                       K_out: Optional[torch.Tensor] = None, Q_win: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Enqueue ecokv_prefill_rope: Q [L][T_total][H_q][D], K [L][T_total][H_kv][D]
+    (views of a fused projection will do) normed and rotated into Q_out, K_out
+    (contiguous; K_out is ecokv_prefill_write's K_new) and the window's queries
+    into Q_win [L][H_q][B][w][D].  Q without Q_out: only the window's."""
+    c = shape.c
+    if c.num_layers == 0:
+        return
+    x = Q if Q is not None else K
+    if x is None:
+        raise ValueError("Q or K is required")
+    if not isinstance(x, torch.Tensor):
+        raise TypeError("Q and K must be torch tensors")
+    dev, n, D = x.device, shape.ttot, c.head_dim
+    code = _dtype_code(x)
+    qp, qs = _token_rows(Q, "Q", x.dtype, c.num_layers, n, c.num_q_heads, D, dev)
+    kp, ks = _token_rows(K, "K", x.dtype, c.num_layers, n, c.num_kv_heads, D, dev)
+    if (Q is None) != (Q_out is None and Q_win is None) or (K is None) != (K_out is None):
+        raise ValueError("Q goes with Q_out, Q_win or both, K with K_out")
+    one = (x.dtype,)
+    _enqueue(lib.ecokv_prefill_rope, dev, stream, qp, qs, kp, ks, code, ctypes.byref(c), rope._arg(D, x.dtype, dev),
+             _arg(positions, "positions", _I32, n, dev, optional=True),
+             _arg(Q_out, "Q_out", one, c.num_layers * n * c.num_q_heads * D, dev, optional=True),
+             _arg(K_out, "K_out", one, c.num_layers * n * c.num_kv_heads * D, dev, optional=True),
+             _arg(Q_win, "Q_win", one, shape.q_numel(), dev, optional=True))
+
+
+def ecokv_append(Q_new: Optional[torch.Tensor], K_new: torch.Tensor, V_new: torch.Tensor, shape: Shape, rope: Rope,
+                 positions: torch.Tensor, conts: Optional[torch.Tensor], rows: torch.Tensor, tails: Tails,
+                 Q_dec: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Enqueue ecokv_append: new tokens' keys (normed, rotated) and values into
+    the tails, their queries into Q_dec [L][H_q][tokens][D].  Q_new, K_new,
+    V_new: [L][tokens][heads][D], views of a fused projection will do;
+    positions, conts (None: token t continues t), rows: int32 [tokens], rows of
+    -1 mark padding."""
+    c = shape.c
+    if not isinstance(K_new, torch.Tensor):
+        raise TypeError("K_new must be a torch tensor")
+    if c.num_layers == 0:
+        return
+    dev, D, dt = K_new.device, c.head_dim, K_new.dtype
+    n = K_new.shape[-3] if K_new.dim() >= 3 else 0
+    code = _dtype_code(K_new)
+    kp, ks = _token_rows(K_new, "K_new", dt, c.num_layers, n, c.num_kv_heads, D, dev)
+    vp, vs = _token_rows(V_new, "V_new", dt, c.num_layers, n, c.num_kv_heads, D, dev)
+    qp, qs = _token_rows(Q_new, "Q_new", dt, c.num_layers, n, c.num_q_heads, D, dev)
+    if V_new is None:
+        raise ValueError("V_new is required")
+    if (Q_new is None) != (Q_dec is None):
+        raise ValueError("Q_new and Q_dec: both or neither")
+    _enqueue(lib.ecokv_append, dev, stream, qp, qs, kp, ks, vp, vs, code, ctypes.byref(c), rope._arg(D, dt, dev),
+             _arg(positions, "positions", _I32, n, dev), _arg(conts, "conts", _I32, n, dev, optional=True),
+             _arg(rows, "rows", _I32, n, dev), n, tails._arg(shape, dt, dev),
+             _arg(Q_dec, "Q_dec", (dt,), c.num_layers * c.num_q_heads * n * D, dev, optional=True))
+
+
+def _fan(shape: Shape, fan):
+    vals = _flat_ints(fan)
+    if len(vals) != shape.c.num_seqs + 1:
+        raise ValueError("fan has one entry per prompt and one more")
+    return (ctypes.c_int32 * len(vals))(*vals)
+
+
+def ecokv_decode_shared_workspace_size(shape: Shape, fan: Sequence[int], max_count: int, max_tail: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib.ecokv_decode_shared_workspace_size(ctypes.byref(shape.c), _fan(shape, fan), int(max_count),
+                                                  int(max_tail), ctypes.byref(n)))
+    return n.value
+
+
+def ecokv_decode_shared(Q_dec: torch.Tensor, Kc: Optional[torch.Tensor], Vc: Optional[torch.Tensor], shape: Shape,
+                        fan: Sequence[int], counts: Optional[torch.Tensor], offsets: Optional[torch.Tensor],
+                        max_count: int, tails: Optional[Tails], tail_counts: Optional[torch.Tensor], max_tail: int,
+                        O: torch.Tensor, lse: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Enqueue ecokv_decode_shared: one query of each continuation over its
+    prompt's kept rows (`fan`: continuations fan[s] .. fan[s + 1] - 1 continue
+    prompt s) and its own tail.  As for ecokv_decode, the caller guarantees that
+    the rows offsets[u] .. + counts[u] lie inside Kc and Vc."""
+    c = shape.c
+    f = _fan(shape, fan)
+    N, D, dt = int(f[c.num_seqs]), c.head_dim, Q_dec.dtype
+    need = ctypes.c_size_t(0)
+    _check(lib.ecokv_decode_shared_workspace_size(ctypes.byref(c), f, int(max_count), int(max_tail), ctypes.byref(need)))
+    if c.num_layers == 0 or N == 0:
+        return
+    dev, nq = Q_dec.device, c.num_layers * c.num_q_heads * N
+    code = _dtype_code(Q_dec)
+    one, some = (dt,), max_count > 0
+    qp = _arg(Q_dec, "Q_dec", one, nq * D, dev)
+    kp, vp = (_arg(t, n, one, D, dev, optional=not some) for t, n in ((Kc, "Kc"), (Vc, "Vc")))
+    if some and (Kc.numel() % D or Vc.numel() != Kc.numel()):
+        raise ValueError("Kc and Vc must hold the same whole number of rows of head_dim elements")
+    workspace = _workspace(workspace, need.value, dev, stream)
+    tp = None
+    if max_tail > 0:
+        if tails is None:
+            raise ValueError("tails is required")
+        tp = tails._arg(shape, dt, dev)
+    _enqueue(lib.ecokv_decode_shared, dev, stream, qp, kp, vp, code, ctypes.byref(c), f,
+             _arg(counts, "counts", _I32, shape.units, dev, optional=not some),
+             _arg(offsets, "offsets", _I32, shape.units, dev, optional=not some), int(max_count), tp,
+             _arg(tail_counts, "tail_counts", _I32, N, dev, optional=max_tail <= 0), int(max_tail),
+             _arg(O, "O", _F32, nq * D, dev), _arg(lse, "lse", _F32, nq, dev, optional=True),
+             _arg(workspace, "workspace", _U8, need.value, dev), workspace.numel())
 
 
 def ecokv_last_error() -> str:
