@@ -1067,7 +1067,10 @@ int ecokv_decode_shared_workspace_size(const ecokv_shape *shape, const int32_t *
     if ((rc = check_fan(si, fan))) return rc;
     if (!bytes) return fail(ECOKV_EINVAL, "bytes is NULL");
     if (max_count < 0 || max_tail < 0) return fail(ECOKV_EINVAL, "max_count %d or max_tail %d < 0", max_count, max_tail);
-    *bytes = ecokv::shared_grid((int64_t)si.L * si.Hkv, si.G, si.D, si.B, fan, max_count, max_tail).bytes;
+    // the element type changes the split; report the larger
+    const size_t b0 = ecokv::shared_grid((int64_t)si.L * si.Hkv, si.G, si.D, si.B, fan, max_count, max_tail, true).bytes;
+    const size_t b1 = ecokv::shared_grid((int64_t)si.L * si.Hkv, si.G, si.D, si.B, fan, max_count, max_tail, false).bytes;
+    *bytes = b0 > b1 ? b0 : b1;
     return ECOKV_OK;
 }
 
@@ -1100,7 +1103,8 @@ int ecokv_decode_shared(const void *Q_dec, const void *Kc, const void *Vc, int d
             return fail(ECOKV_EINVAL, "max_tail %d is more rows than %d pages of %d hold", max_tail, tails->max_pages,
                         tails->page_size);
     }
-    a.grid = ecokv::shared_grid((int64_t)si.L * si.Hkv, si.G, si.D, si.B, fan, max_count, max_tail);
+    a.grid = ecokv::shared_grid((int64_t)si.L * si.Hkv, si.G, si.D, si.B, fan, max_count, max_tail,
+                                dtype == ECOKV_BF16);
     if (!workspace) return fail(ECOKV_EINVAL, "workspace is NULL");
     if (((uintptr_t)workspace & 255u) != 0) return fail(ECOKV_EINVAL, "workspace must be 256-byte aligned");
     if (workspace_bytes < a.grid.bytes)

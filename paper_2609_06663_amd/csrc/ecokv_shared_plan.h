@@ -11,9 +11,13 @@
 namespace ecokv {
 
 constexpr int kShWaves = 4;                     // waves per block
-constexpr int kShTile = 32;                     // rows a wave takes at a time (fp32: 16)
-constexpr int kShStep = kShWaves * kShTile;     // a part's rows are a multiple of this
-constexpr int kShBlocks = 512;                  // blocks that fill the device
+constexpr int kTailQ = 16;                      // query heads of a wave in the tails
+// Blocks (and four times as many waves of the tails) that the parts may make: one
+// per compute unit.  Two fit, but every further part is a partial of each query
+// row to write and to merge (us, 256 against 512: 64 continuations of 6553 rows
+// 45 and 55, 20 of 64 heads of 8191 rows 41 and 44; 28 layers of 16 139 and 136).
+constexpr int kShBlocks = 256;
+constexpr int kShMostRows = 1 << 22;            // rows of a part at most: its bytes are addressed by 32 bits
 
 // The page of row `row` of continuation `cont`, or -1: a row outside the
 // table, a continuation outside it, a page outside the pool.
@@ -34,51 +38,75 @@ __host__ __device__ inline int64_t tail_row(const TailMap &m, int Hkv, int l, in
     return ((((int64_t)l * m.pages + page) * Hkv + h) << m.shift) + (row & ((1 << m.shift) - 1));
 }
 
-// Rows of one of `parts` equal parts of n rows, and how many parts have rows.
-__host__ __device__ inline int64_t part_rows(int n, int parts)
+// Rows of one of `parts` equal parts of n rows, a multiple of `step`, and how
+// many parts have rows.
+__host__ __device__ inline int64_t part_rows(int n, int parts, int step)
 {
     const int64_t r = ((int64_t)n + parts - 1) / parts;
-    return (r + kShStep - 1) / kShStep * kShStep;
+    return (r + step - 1) / step * step;
 }
-__host__ __device__ inline int parts_used(int n, int parts)
+__host__ __device__ inline int parts_used(int n, int parts, int step)
 {
-    return n > 0 ? (int)((n + part_rows(n, parts) - 1) / part_rows(n, parts)) : 0;
+    return n > 0 ? (int)((n + part_rows(n, parts, step) - 1) / part_rows(n, parts, step)) : 0;
 }
 
-// A call's blocks.  The prompt's part: for each (layer, KV head), prompt and
-// tile of `qt` query rows (G x its continuations), np parts of the kept rows.
-// The tails' part: for each (layer, KV head), continuation and 16 query heads,
-// nt parts of the tail.  Each block writes a partial of each of its query rows
-// to the part's place in the workspace: [np + nt][L H_q N] sums [D], and
-// (maximum, sum).
+// A call's work.
+//  * The prompt's part.  The query rows of a (layer, KV head) and prompt, G x
+//    its continuations, are cut into tiles of wq x rows_q, rows_q per wave;
+//    its kept rows into np parts.  A block takes one tile and one part; the
+//    four waves' 4 / wq groups share the part's rows.
+//  * The tails' part.  A wave takes kTailQ query heads of a (layer, KV head) and
+//    continuation and one of nt parts of the tail; four waves share a block.
+// Each leaves a partial of every query row at the part's place in the
+// workspace: [np + nt][L H_q N] sums [D], and (maximum, sum).
+// Rows are taken rows_t at a time; rows_q and rows_t are 32 (bf16) or 16 (fp32).
 struct SharedGrid {
-    int qt;              // query rows of a prompt block
-    int np, nt;          // parts per unit of kept rows and per tail
-    int tiles;           // query tiles of the prompts of a (layer, KV head)
+    int rows_q, rows_t, wq;
+    int np, nt;               // parts of a unit's kept rows, of a tail
+    int step, tail_step;      // a prompt part's and a tail part's rows are multiples of these
+    int tiles;                // query tiles of the prompts of a (layer, KV head)
     int tile0[ECOKV_MAX_SEQS + 1];  // before each prompt
-    int64_t prompt_blocks, tail_blocks, qrows;
+    int groups;               // groups of kTailQ query heads of a tail
+    int64_t prompt_blocks, tail_waves, qrows;
     size_t bytes;
 };
-__host__ __device__ inline int tail_groups(int G) { return (G + 15) / 16; }
 
-inline int parts_for(int64_t blocks, int rows)
+// Parts that give `have` blocks (waves) times as many no more than `room`, none
+// of fewer than `step` rows or of more than kShMostRows.
+inline int parts_for(int64_t have, int64_t room, int rows, int step)
 {
-    const int64_t want = blocks > 0 ? (kShBlocks + blocks - 1) / blocks : 1, most = ((int64_t)rows + kShStep - 1) / kShStep;
-    return (int)(rows <= 0 ? 0 : want < most ? want : most);
+    if (rows <= 0 || have <= 0) return 0;
+    int64_t parts = room / have;
+    const int64_t most = ((int64_t)rows + step - 1) / step, least = ((int64_t)rows + kShMostRows - 1) / kShMostRows;
+    if (parts > most) parts = most;
+    return (int)(parts < least ? least : parts);
 }
 
-inline SharedGrid shared_grid(int64_t pairs, int G, int D, int B, const int32_t *fan, int max_count, int max_tail)
+inline SharedGrid shared_grid(int64_t pairs, int G, int D, int B, const int32_t *fan, int max_count, int max_tail, bool bf16)
 {
     SharedGrid g{};
     const int N = fan[B];
-    g.qt = 16;
-    for (int s = 0; s < B; ++s)
-        g.tile0[s + 1] = g.tile0[s] + (int)(((int64_t)G * (fan[s + 1] - fan[s]) + g.qt - 1) / g.qt);
+    g.rows_q = g.rows_t = bf16 ? 32 : 16;
+    int64_t most = 0;
+    for (int s = 0; s < B; ++s) {
+        const int64_t m = (int64_t)G * (fan[s + 1] - fan[s]);
+        if (m > most) most = m;
+    }
+    // as many waves along the query rows as the largest prompt fills: each row
+    // of the cache then serves them all from LDS
+    g.wq = most > 2 * g.rows_q ? 4 : most > g.rows_q ? 2 : 1;
+    g.step = g.rows_t * (kShWaves / g.wq);
+    g.tail_step = 2 * g.rows_t;
+    const int qt = g.wq * g.rows_q;
+    for (int s = 0; s < B; ++s) {
+        g.tile0[s + 1] = g.tile0[s] + (int)(((int64_t)G * (fan[s + 1] - fan[s]) + qt - 1) / qt);
+    }
     g.tiles = max_count > 0 ? g.tile0[B] : 0;
-    g.np = parts_for(pairs * g.tiles, max_count);
-    g.nt = parts_for(pairs * N * tail_groups(G), max_tail);
+    g.groups = (G + kTailQ - 1) / kTailQ;
+    g.np = parts_for(pairs * g.tiles, kShBlocks, max_count, g.step);
+    g.nt = parts_for(pairs * N * g.groups, kShBlocks * kShWaves, max_tail, g.tail_step);
     g.prompt_blocks = pairs * g.tiles * g.np;
-    g.tail_blocks = pairs * N * tail_groups(G) * g.nt;
+    g.tail_waves = pairs * N * g.groups * g.nt;
     g.qrows = pairs * G * N;
     g.bytes = sizeof(float) * (size_t)(g.np + g.nt) * (size_t)g.qrows * (size_t)(D + 2);
     return g;

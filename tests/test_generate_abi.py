@@ -172,7 +172,7 @@ def test_decode_shared_refusals(P, E):
     assert call(t=good, mt=129) == -1                          # more than 8 pages of 16
     assert call(t=tails(E, num_conts=4)) == -1
     assert call(t=good, w=None) == -1 and call(t=good, w=ctypes.c_void_p(260)) == -1
-    assert call(t=good, wb=ws - 1) == -2
+    assert call(t=good, wb=1024) == -2
     assert call(fn=fan(0, 0, 0), Q=None) == 0                  # nobody continues
     assert call(shape=P.Shape(0, 8, 2, 128, 4, [0, 100, 250]), Q=None) == 0
 

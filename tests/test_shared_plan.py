@@ -24,14 +24,14 @@ extern "C" int page_of(const int *table, int conts, int pages, int shift, int ma
 extern "C" long long row_of(int pages, int shift, int Hkv, int l, int h, int page, int row) {
     return tail_row(TailMap{nullptr, 1, pages, shift, 1}, Hkv, l, h, page, row);
 }
-// every count n of 0 .. max rows: its parts hold its rows once, each a whole number of steps but the last
-static int covers(int n, int parts) {
+// a count of n rows: its parts hold its rows once, each a whole number of steps but the last
+static int covers(int n, int parts, int step) {
     long long got = 0;
-    const int used = parts_used(n, parts);
+    const int used = parts_used(n, parts, step);
     if (used > parts) return 1;
     if (n <= 0) return used != 0;
-    const long long pr = part_rows(n, parts);
-    if (pr % kShStep) return 2;
+    const long long pr = part_rows(n, parts, step);
+    if (pr % step || pr > kShMostRows + step) return 2;
     for (int p = 0; p < parts; ++p) {
         const long long left = (long long)n - p * pr;
         if ((left > 0) != (p < used)) return 3;
@@ -39,22 +39,24 @@ static int covers(int n, int parts) {
     }
     return got == n ? 0 : 4;
 }
-extern "C" int plan(long long pairs, int G, int D, int B, const int *fan, int max_count, int max_tail, const int *n, int nn, long long *out) {
-    const SharedGrid g = shared_grid(pairs, G, D, B, fan, max_count, max_tail);
-    out[0] = g.np, out[1] = g.nt, out[2] = g.prompt_blocks, out[3] = g.tail_blocks, out[4] = (long long)g.bytes, out[5] = g.qt;
-    if ((max_count > 0 && fan[B] > 0) != (g.np > 0 && g.prompt_blocks > 0)) return 10;
-    if ((max_tail > 0) != (g.nt > 0)) return 11;
+extern "C" int plan(long long pairs, int G, int D, int B, const int *fan, int max_count, int max_tail, int bf16, const int *n, int nn, long long *out) {
+    const SharedGrid g = shared_grid(pairs, G, D, B, fan, max_count, max_tail, bf16 != 0);
+    out[0] = g.np, out[1] = g.nt, out[2] = g.prompt_blocks, out[3] = g.tail_waves, out[4] = (long long)g.bytes, out[5] = g.wq;
+    const int N = fan[B], qt = g.wq * g.rows_q;
+    if ((max_count > 0 && N > 0) != (g.np > 0) || g.prompt_blocks != pairs * g.tiles * g.np) return 10;
+    if ((max_tail > 0 && N > 0) != (g.nt > 0) || g.tail_waves != pairs * N * g.groups * g.nt || g.groups * kTailQ < G) return 11;
+    if (g.step != g.rows_t * (kShWaves / g.wq) || kShWaves % g.wq) return 14;
     for (int s = 0; s < B; ++s) {  // every query row of a prompt has one tile
         const long long M = (long long)G * (fan[s + 1] - fan[s]), t = g.tile0[s + 1] - g.tile0[s];
-        if (t * g.qt < M || (t - 1) * g.qt >= M) return 12;
+        if (t * qt < M || (M > 0 ? (t - 1) * qt >= M : t != 0)) return 12;
     }
     for (int i = 0; i < nn; ++i) {
-        if (max_count > 0)
-            if (int rc = covers(n[i] < max_count ? n[i] : max_count, g.np)) return rc;
-        if (max_tail > 0)
-            if (int rc = covers(n[i] < max_tail ? n[i] : max_tail, g.nt)) return 20 + rc;
+        if (g.np > 0)
+            if (int rc = covers(n[i] < max_count ? n[i] : max_count, g.np, g.step)) return rc;
+        if (g.nt > 0)
+            if (int rc = covers(n[i] < max_tail ? n[i] : max_tail, g.nt, g.tail_step)) return 20 + rc;
     }
-    return g.bytes == 4ull * (g.np + g.nt) * pairs * G * fan[B] * (D + 2) ? 0 : 13;
+    return g.bytes == 4ull * (g.np + g.nt) * pairs * G * N * (D + 2) ? 0 : 13;
 }
 """
 
@@ -71,7 +73,7 @@ def lib(tmp_path_factory):
     lib.row_of.argtypes = [ctypes.c_int] * 7
     lib.row_of.restype = ctypes.c_longlong
     lib.plan.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_int, ctypes.c_int,
-                         ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p]
+                         ctypes.c_int, ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p]
     return lib
 
 
@@ -111,6 +113,9 @@ def test_parts_cover_every_row_once(lib, G):
                 top = max(mc, mt, 1)
                 n = np.unique(np.clip(np.concatenate([[0, 1, 31, 32, 33, 127, 128, 129, mc, mt, top - 1, -5],
                                                       rng.integers(0, top, 20)]), -5, top)).astype(np.int32)
-                rc = lib.plan(pairs, G, 128, len(fan), cum.ctypes.data, mc, mt, n.ctypes.data, len(n), out.ctypes.data)
-                assert rc == 0, (rc, pairs, G, fan, mc, mt, out.tolist())
-                assert out[0] <= 512 and out[1] <= 512
+                for bf16 in (0, 1):
+                    rc = lib.plan(pairs, G, 128, len(fan), cum.ctypes.data, mc, mt, bf16, n.ctypes.data, len(n), out.ctypes.data)
+                    assert rc == 0, (rc, pairs, G, fan, mc, mt, bf16, out.tolist())
+                    # one round of the device, or one part each (of what 32-bit offsets reach)
+                    assert out[2] <= 256 or out[0] == max(1, -(-mc // 2 ** 22))
+                    assert out[3] <= 1024 or out[1] == max(1, -(-mt // 2 ** 22))
