@@ -123,18 +123,24 @@ class _Rope(ctypes.Structure):
 class Rope:
     """ecokv_rope: rotary positions (`freq` float32 [rot_dim / 2], see
     ecokv_rope_freqs) and, where `q_norm` / `k_norm` [D] weights are given, the
-    per-head norms before them.  Holds the tensors that it points to."""
+    per-head norms before them.  Holds the tensors that it points to, whose
+    values may change but not their storage."""
 
     def __init__(self, rot_dim: int, freq: Optional[torch.Tensor] = None, interleaved: bool = False, factor: float = 1.0,
                  q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, norm_eps: float = 1e-6):
         self.freq, self.q_norm, self.k_norm = freq, q_norm, k_norm
         self.c = _Rope(int(rot_dim), int(bool(interleaved)), None, factor, norm_eps, None, None)
 
+        self._for = None
+
     def _arg(self, head_dim: int, dtype, device):
-        """Pointer to the checked structure, for rows of this element type."""
-        self.c.freq = _arg(self.freq, "freq", _F32, max(self.c.rot_dim, 0) // 2, device, optional=self.c.rot_dim <= 0)
-        self.c.q_norm = _arg(self.q_norm, "q_norm", (dtype,), head_dim, device, optional=True)
-        self.c.k_norm = _arg(self.k_norm, "k_norm", (dtype,), head_dim, device, optional=True)
+        """Pointer to the structure, checked for rows of this size, element type and
+        device when these differ from the last call's."""
+        if self._for != (head_dim, dtype, device):
+            self.c.freq = _arg(self.freq, "freq", _F32, max(self.c.rot_dim, 0) // 2, device, optional=self.c.rot_dim <= 0)
+            self.c.q_norm = _arg(self.q_norm, "q_norm", (dtype,), head_dim, device, optional=True)
+            self.c.k_norm = _arg(self.k_norm, "k_norm", (dtype,), head_dim, device, optional=True)
+            self._for = head_dim, dtype, device
         return ctypes.byref(self.c)
 
 
@@ -146,7 +152,8 @@ class _Tails(ctypes.Structure):
 
 class Tails:
     """ecokv_tails: K, V [L][num_pages][H_kv][page_size][D] and table (int32)
-    [num_conts][max_pages].  Holds the tensors that it points to."""
+    [num_conts][max_pages].  Holds the tensors that it points to, whose values
+    may change but not their storage."""
 
     def __init__(self, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor):
         if K.dim() != 5 or V.shape != K.shape or V.dtype != K.dtype:
@@ -156,16 +163,22 @@ class Tails:
         self.K, self.V, self.table = K, V, table
         self.c = _Tails(None, None, None, table.shape[0], K.shape[1], K.shape[3], table.shape[1])
 
+        self._for = None
+
     def _arg(self, shape: "Shape", dtype, device):
-        """Pointer to the checked structure, for calls of this shape and element type."""
+        """Pointer to the structure, checked for calls of this shape, element type
+        and device when these differ from the last call's."""
         c = shape.c
-        L, _, H, _, D = self.K.shape
-        if (L, H, D) != (c.num_layers, c.num_kv_heads, c.head_dim):
-            raise ValueError(f"the tails have {L} layers of {H} KV heads of {D} dimensions, the shape "
-                             f"{c.num_layers} of {c.num_kv_heads} of {c.head_dim}")
-        self.c.K = _arg(self.K, "the tails' K", (dtype,), self.K.numel(), device)
-        self.c.V = _arg(self.V, "the tails' V", (dtype,), self.K.numel(), device)
-        self.c.table = _arg(self.table, "the tails' table", _I32, self.table.numel(), device)
+        now = c.num_layers, c.num_kv_heads, c.head_dim, dtype, device
+        if self._for != now:
+            L, _, H, _, D = self.K.shape
+            if (L, H, D) != now[:3]:
+                raise ValueError(f"the tails have {L} layers of {H} KV heads of {D} dimensions, the shape "
+                                 f"{c.num_layers} of {c.num_kv_heads} of {c.head_dim}")
+            self.c.K = _arg(self.K, "the tails' K", (dtype,), self.K.numel(), device)
+            self.c.V = _arg(self.V, "the tails' V", (dtype,), self.K.numel(), device)
+            self.c.table = _arg(self.table, "the tails' table", _I32, self.table.numel(), device)
+            self._for = now
         return ctypes.byref(self.c)
 
 
@@ -572,39 +585,62 @@ def ecokv_decode(Q_dec: torch.Tensor, Kc: torch.Tensor, Vc: torch.Tensor, shape:
 
 def _enqueue(fn, device, stream, *args):
     """fn(*args, stream) on `stream` or the current stream of the tensors' device."""
-    if stream is not None and stream.device != device:
-        raise ValueError(f"the stream is on {stream.device}, the call's tensors on {device}")
+    if stream is not None:
+        if stream.device != device:
+            raise ValueError(f"the stream is on {stream.device}, the call's tensors on {device}")
+        raw = stream.cuda_stream
+    else:
+        raw = torch._C._cuda_getCurrentRawStream(device.index)
     if device.index == torch._C._cuda_getDevice():
-        _check(fn(*args, _stream(stream)))
+        _check(fn(*args, raw))
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, _stream(stream)))
+            _check(fn(*args, raw))
 
 
-def _token_rows(t: Optional[torch.Tensor], name: str, dtype, layers: int, tokens: int, heads: int, dim: int, device):
-    """(pointer, stride) of rows [L][tokens][heads][dim] (or, for one layer,
-    [tokens][heads][dim]) that may lie further apart than they are long: a view
-    of a fused projection's output, say."""
-    if t is None:
-        return None, 0
+def _fit(t: Optional[torch.Tensor], name: str, dtype, numel: int, device, optional: bool = False):
+    """_arg for one element type: a call in order costs fewer Python steps."""
+    if t is None and optional:
+        return None
+    try:
+        if t.get_device() == device.index and t.dtype is dtype and t.numel() >= numel and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    return _arg(t, name, (dtype,), numel, device, optional)
+
+
+def _first(t, name: str):
+    """Device and element type of the tensor that the call's others are held to."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor (got {t.device})")
-    if t.device != device:
+    return t.device, t.dtype, _dtype_code(t)
+
+
+def _token_rows(t: Optional[torch.Tensor], name: str, dtype, want, device):
+    """(pointer, stride) of rows `want` = (L, tokens, heads, dim) (or, for one
+    layer, without L) that may lie further apart than they are long: a view of a
+    fused projection's output, say."""
+    if t is None:
+        return None, 0
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.get_device() != device.index:
         raise ValueError(f"{name} is on {t.device}, the call's tensors on {device}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {_ELEM.get(dtype, str(dtype))} (got {t.dtype})")
-    want = (layers, tokens, heads, dim)
-    if tuple(t.shape) != want and not (layers == 1 and tuple(t.shape) == want[1:]):
+    layers, tokens, heads, dim = want
+    if t.shape != want and not (layers == 1 and t.shape == want[1:]):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, the call needs {want}")
     packed = heads * dim
     s = t.stride()
     stride = s[-3] if tokens > 1 else s[0] if layers > 1 else packed
-    if t.numel() and ((dim > 1 and s[-1] != 1) or (heads > 1 and s[-2] != dim)
-                      or (layers > 1 and s[0] != tokens * stride)):
+    if tokens and ((dim > 1 and s[-1] != 1) or (heads > 1 and s[-2] != dim)
+                   or (layers > 1 and s[0] != tokens * stride)):
         raise ValueError(f"{name}: the heads of a token must lie together and the tokens of all layers evenly apart")
-    return t.data_ptr(), max(stride, packed) if not t.numel() else stride
+    return t.data_ptr(), stride if tokens else packed
 
 
 def ecokv_rope_freqs(rot_dim: int, base: float = 10000.0, kind: int = ROPE_PLAIN, stretch: float = 1.0,
@@ -627,23 +663,18 @@ def ecokv_prefill_rope(Q: Optional[torch.Tensor], K: Optional[torch.Tensor], sha
     c = shape.c
     if c.num_layers == 0:
         return
-    x = Q if Q is not None else K
-    if x is None:
+    if Q is None and K is None:
         raise ValueError("Q or K is required")
-    if not isinstance(x, torch.Tensor):
-        raise TypeError("Q and K must be torch tensors")
-    dev, n, D = x.device, shape.ttot, c.head_dim
-    code = _dtype_code(x)
-    qp, qs = _token_rows(Q, "Q", x.dtype, c.num_layers, n, c.num_q_heads, D, dev)
-    kp, ks = _token_rows(K, "K", x.dtype, c.num_layers, n, c.num_kv_heads, D, dev)
     if (Q is None) != (Q_out is None and Q_win is None) or (K is None) != (K_out is None):
         raise ValueError("Q goes with Q_out, Q_win or both, K with K_out")
-    one = (x.dtype,)
-    _enqueue(lib.ecokv_prefill_rope, dev, stream, qp, qs, kp, ks, code, ctypes.byref(c), rope._arg(D, x.dtype, dev),
-             _arg(positions, "positions", _I32, n, dev, optional=True),
-             _arg(Q_out, "Q_out", one, c.num_layers * n * c.num_q_heads * D, dev, optional=True),
-             _arg(K_out, "K_out", one, c.num_layers * n * c.num_kv_heads * D, dev, optional=True),
-             _arg(Q_win, "Q_win", one, shape.q_numel(), dev, optional=True))
+    dev, dt, code = _first(Q if Q is not None else K, "Q" if Q is not None else "K")
+    L, Hq, Hkv, D, n = c.num_layers, c.num_q_heads, c.num_kv_heads, c.head_dim, shape.ttot
+    qp, qs = _token_rows(Q, "Q", dt, (L, n, Hq, D), dev)
+    kp, ks = _token_rows(K, "K", dt, (L, n, Hkv, D), dev)
+    _enqueue(lib.ecokv_prefill_rope, dev, stream, qp, qs, kp, ks, code, ctypes.byref(c), rope._arg(D, dt, dev),
+             _fit(positions, "positions", torch.int32, n, dev, True), _fit(Q_out, "Q_out", dt, L * n * Hq * D, dev, True),
+             _fit(K_out, "K_out", dt, L * n * Hkv * D, dev, True),
+             _fit(Q_win, "Q_win", dt, shape.q_numel() if Q_win is not None else 0, dev, True))
 
 
 def ecokv_append(Q_new: Optional[torch.Tensor], K_new: torch.Tensor, V_new: torch.Tensor, shape: Shape, rope: Rope,
@@ -655,31 +686,31 @@ def ecokv_append(Q_new: Optional[torch.Tensor], K_new: torch.Tensor, V_new: torc
     positions, conts (None: token t continues t), rows: int32 [tokens], rows of
     -1 mark padding."""
     c = shape.c
-    if not isinstance(K_new, torch.Tensor):
-        raise TypeError("K_new must be a torch tensor")
     if c.num_layers == 0:
         return
-    dev, D, dt = K_new.device, c.head_dim, K_new.dtype
-    n = K_new.shape[-3] if K_new.dim() >= 3 else 0
-    code = _dtype_code(K_new)
-    kp, ks = _token_rows(K_new, "K_new", dt, c.num_layers, n, c.num_kv_heads, D, dev)
-    vp, vs = _token_rows(V_new, "V_new", dt, c.num_layers, n, c.num_kv_heads, D, dev)
-    qp, qs = _token_rows(Q_new, "Q_new", dt, c.num_layers, n, c.num_q_heads, D, dev)
     if V_new is None:
         raise ValueError("V_new is required")
     if (Q_new is None) != (Q_dec is None):
         raise ValueError("Q_new and Q_dec: both or neither")
+    dev, dt, code = _first(K_new, "K_new")
+    L, Hq, Hkv, D = c.num_layers, c.num_q_heads, c.num_kv_heads, c.head_dim
+    n = K_new.shape[-3] if K_new.dim() >= 3 else 0
+    kp, ks = _token_rows(K_new, "K_new", dt, (L, n, Hkv, D), dev)
+    vp, vs = _token_rows(V_new, "V_new", dt, (L, n, Hkv, D), dev)
+    qp, qs = _token_rows(Q_new, "Q_new", dt, (L, n, Hq, D), dev)
     _enqueue(lib.ecokv_append, dev, stream, qp, qs, kp, ks, vp, vs, code, ctypes.byref(c), rope._arg(D, dt, dev),
-             _arg(positions, "positions", _I32, n, dev), _arg(conts, "conts", _I32, n, dev, optional=True),
-             _arg(rows, "rows", _I32, n, dev), n, tails._arg(shape, dt, dev),
-             _arg(Q_dec, "Q_dec", (dt,), c.num_layers * c.num_q_heads * n * D, dev, optional=True))
+             _fit(positions, "positions", torch.int32, n, dev), _fit(conts, "conts", torch.int32, n, dev, True),
+             _fit(rows, "rows", torch.int32, n, dev), n, tails._arg(shape, dt, dev),
+             _fit(Q_dec, "Q_dec", dt, L * Hq * n * D, dev, True))
 
 
 def _fan(shape: Shape, fan):
-    vals = _flat_ints(fan)
-    if len(vals) != shape.c.num_seqs + 1:
-        raise ValueError("fan has one entry per prompt and one more")
-    return (ctypes.c_int32 * len(vals))(*vals)
+    n = shape.c.num_seqs + 1
+    if not (type(fan) is list and len(fan) == n):
+        fan = _flat_ints(fan)
+        if len(fan) != n:
+            raise ValueError("fan has one entry per prompt and one more")
+    return (ctypes.c_int32 * n)(*fan)
 
 
 def ecokv_decode_shared_workspace_size(shape: Shape, fan: Sequence[int], max_count: int, max_tail: int) -> int:
@@ -700,30 +731,28 @@ def ecokv_decode_shared(Q_dec: torch.Tensor, Kc: Optional[torch.Tensor], Vc: Opt
     the rows offsets[u] .. + counts[u] lie inside Kc and Vc."""
     c = shape.c
     f = _fan(shape, fan)
-    N, D, dt = int(f[c.num_seqs]), c.head_dim, Q_dec.dtype
-    need = ctypes.c_size_t(0)
-    _check(lib.ecokv_decode_shared_workspace_size(ctypes.byref(c), f, int(max_count), int(max_tail), ctypes.byref(need)))
+    N = f[c.num_seqs]
     if c.num_layers == 0 or N == 0:
         return
-    dev, nq = Q_dec.device, c.num_layers * c.num_q_heads * N
-    code = _dtype_code(Q_dec)
-    one, some = (dt,), max_count > 0
-    qp = _arg(Q_dec, "Q_dec", one, nq * D, dev)
-    kp, vp = (_arg(t, n, one, D, dev, optional=not some) for t, n in ((Kc, "Kc"), (Vc, "Vc")))
-    if some and (Kc.numel() % D or Vc.numel() != Kc.numel()):
+    dev, dt, code = _first(Q_dec, "Q_dec")
+    D = c.head_dim
+    nq = c.num_layers * c.num_q_heads * N
+    kept, tailed = max_count > 0, max_tail > 0
+    qp = _fit(Q_dec, "Q_dec", dt, nq * D, dev)
+    kp, vp = _fit(Kc, "Kc", dt, D, dev, not kept), _fit(Vc, "Vc", dt, D, dev, not kept)
+    if kept and (Kc.numel() % D or Vc.numel() != Kc.numel()):
         raise ValueError("Kc and Vc must hold the same whole number of rows of head_dim elements")
-    workspace = _workspace(workspace, need.value, dev, stream)
-    tp = None
-    if max_tail > 0:
-        if tails is None:
-            raise ValueError("tails is required")
-        tp = tails._arg(shape, dt, dev)
+    if tailed and tails is None:
+        raise ValueError("tails is required")
+    if workspace is None:
+        workspace = _workspace(None, ecokv_decode_shared_workspace_size(shape, fan, max_count, max_tail), dev, stream)
+    units = shape.units
     _enqueue(lib.ecokv_decode_shared, dev, stream, qp, kp, vp, code, ctypes.byref(c), f,
-             _arg(counts, "counts", _I32, shape.units, dev, optional=not some),
-             _arg(offsets, "offsets", _I32, shape.units, dev, optional=not some), int(max_count), tp,
-             _arg(tail_counts, "tail_counts", _I32, N, dev, optional=max_tail <= 0), int(max_tail),
-             _arg(O, "O", _F32, nq * D, dev), _arg(lse, "lse", _F32, nq, dev, optional=True),
-             _arg(workspace, "workspace", _U8, need.value, dev), workspace.numel())
+             _fit(counts, "counts", torch.int32, units, dev, not kept), _fit(offsets, "offsets", torch.int32, units, dev, not kept),
+             int(max_count), tails._arg(shape, dt, dev) if tailed else None,
+             _fit(tail_counts, "tail_counts", torch.int32, N, dev, not tailed), int(max_tail),
+             _fit(O, "O", torch.float32, nq * D, dev), _fit(lse, "lse", torch.float32, nq, dev, True),
+             _fit(workspace, "workspace", torch.uint8, 0, dev), workspace.numel())
 
 
 def ecokv_last_error() -> str:

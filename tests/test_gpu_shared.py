@@ -293,6 +293,6 @@ def test_the_binding_refuses_what_does_not_fit():
     for kw, err in ((dict(Q=c.Q[:, :3]), ValueError), (dict(K=c.Kc.float()), TypeError), (dict(V=c.Vc[:-1]), ValueError), (dict(n=c.counts.long()), TypeError),
                     (dict(o=c.offsets[:1]), ValueError), (dict(t=None), ValueError), (dict(tc=None), ValueError), (dict(tc=c.tail_counts[:1]), ValueError),
                     (dict(O=O.bfloat16()), TypeError), (dict(O=O[:, :3]), ValueError), (dict(lse=lse[:, :3]), ValueError), (dict(K=None), ValueError),
-                    (dict(ws=torch.empty(64, dtype=torch.uint8, device="cuda")), ValueError), (dict(fan=[0, 1]), P.EcoKVError), (dict(mt=17), P.EcoKVError)):
+                    (dict(ws=torch.empty(256, dtype=torch.uint8, device="cuda")), P.EcoKVError), (dict(ws=torch.empty(256, device="cuda")), TypeError), (dict(fan=[0, 1]), P.EcoKVError), (dict(mt=17), P.EcoKVError)):
         with pytest.raises(err):
             call(**kw)
