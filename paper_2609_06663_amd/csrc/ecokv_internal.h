@@ -234,7 +234,7 @@ struct RopeArgs {
     int rot, interleaved;
     int L, n, Hq, Hkv, B, w;
     int hq, hk;           // query and KV heads that the call handles (0: none)
-    int per_block;        // tokens per block
+    int split;            // a block per token, its heads dealt to the waves (else a wave per token)
     TailMap map;
     SeqTab seq;
 };

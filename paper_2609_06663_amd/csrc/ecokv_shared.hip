@@ -49,49 +49,52 @@ struct SharedItem {
 __device__ __forceinline__ void item_rows(SharedItem &it, int n, int most, int parts, int part, int step)
 {
     n = n < 0 || n > most ? 0 : n;  // (counts out of their bounds: the merge writes NaN)
-    const int64_t pr = part_rows(n, parts, step);
-    it.row0 = (int)min(part * pr, (int64_t)n);
-    it.rows = (int)min((int64_t)(n - it.row0), pr);
+    const uint32_t pr = part_rows(n, parts, step);
+    const uint64_t r0 = (uint64_t)(uint32_t)part * pr;
+    it.row0 = uniform_i32((int)min(r0, (uint64_t)n));
+    it.rows = uniform_i32((int)min((uint32_t)(n - it.row0), pr));
 }
 
-__device__ __forceinline__ void prompt_item(const SharedArgs &a, int64_t b, SharedItem &it)
+__device__ __forceinline__ void prompt_item(const SharedArgs &a, uint32_t b, SharedItem &it)
 {
     const SharedGrid &g = a.grid;
-    const int per = g.tiles * g.np, qt = g.wq * g.rows_q;
-    const int lh = (int)(b / per), r = (int)(b - (int64_t)lh * per);
-    const int part = r / g.tiles, tile = r - part * g.tiles;
+    const uint32_t per = (uint32_t)(g.tiles * g.np);
+    const int qt = g.wq * g.rows_q;
+    const int lh = (int)(b / per), r = (int)(b - (uint32_t)lh * per);
+    const int part = (int)((uint32_t)r / (uint32_t)g.tiles), tile = r - part * g.tiles;
     int s = 0;
     while (s + 1 < a.B && g.tile0[s + 1] <= tile) ++s;
+    const int64_t u = (int64_t)lh * a.B + s;
+    const int n = uniform_i32(a.counts[u]), off = uniform_i32(a.offsets[u]);
     it.c0 = a.fan[s];
     it.nc = a.fan[s + 1] - it.c0;
     it.q0 = (tile - g.tile0[s]) * qt;
     it.nq = min(qt, a.G * it.nc - it.q0);
-    it.l = lh / a.Hkv;
+    it.l = (int)((uint32_t)lh / (uint32_t)a.Hkv);
     it.h = lh - it.l * a.Hkv;
     it.part = part;
-    const int64_t u = (int64_t)lh * a.B + s;
-    const int n = uniform_i32(a.counts[u]);
-    it.base = uniform_i32(a.offsets[u]);
+    it.base = off;
     item_rows(it, n, a.max_count, g.np, part, g.step);
 }
 
-__device__ __forceinline__ void tail_item(const SharedArgs &a, int64_t w, SharedItem &it)
+__device__ __forceinline__ void tail_item(const SharedArgs &a, uint32_t w, SharedItem &it)
 {
     const SharedGrid &g = a.grid;
-    const int64_t e = w / g.nt;
-    const int part = (int)(w - e * g.nt);
-    const int64_t f = e / g.groups;
-    const int z = (int)(e - f * g.groups);
-    const int lh = (int)(f / a.N);
-    it.c0 = (int)(f - (int64_t)lh * a.N);
+    const uint32_t e = w / (uint32_t)g.nt;
+    const int part = (int)(w - e * (uint32_t)g.nt);
+    const uint32_t f = g.groups == 1 ? e : e / (uint32_t)g.groups;
+    const int z = (int)(e - f * (uint32_t)g.groups);
+    const int lh = (int)(f / (uint32_t)a.N);
+    it.c0 = (int)(f - (uint32_t)lh * (uint32_t)a.N);
+    const int n = uniform_i32(a.tail_counts[it.c0]);
     it.nc = 1;
     it.q0 = z * kTailQ;
     it.nq = min(kTailQ, a.G - it.q0);
-    it.l = lh / a.Hkv;
+    it.l = (int)((uint32_t)lh / (uint32_t)a.Hkv);
     it.h = lh - it.l * a.Hkv;
     it.part = g.np + part;
     it.base = 0;
-    item_rows(it, uniform_i32(a.tail_counts[it.c0]), a.max_tail, g.nt, part, g.tail_step);
+    item_rows(it, n, a.max_tail, g.nt, part, g.tail_step);
 }
 
 // Shapes of a wave's work: QT query rows (bf16 32 or 16, fp32 16) and a tile of
@@ -506,11 +509,14 @@ __device__ __forceinline__ void prompt_part(const SharedArgs &a, const SharedIte
 #pragma unroll
             for (int i = 0; i < Ge::NL; ++i) to[stage_chunk<BF, Ge::S>(Ge::RPI * i + lane / Ge::S, lane % Ge::S)] = x[i];
         };
-        load(kx, rk, 0);
-        load(vx, rv, 0);
-        load_queries<BF, D, QT>(a, it, q0, nq, w);
-        put(kx, stage);
-        load(kx, rk, 1);
+        {  // (the first tiles' loads together: one round trip)
+            u32x4s k0[Ge::NL];
+            load(k0, rk, 0);
+            load(kx, rk, 1);
+            load(vx, rv, 0);
+            load_queries<BF, D, QT>(a, it, q0, nq, w);
+            put(k0, stage);
+        }
         typename Ge::X x, y;
         first_tile<BF, D, QT>(stage, x, nrows, 0u, a.qscale, w);
         for (int t = 0; t * Ge::TR < nrows; ++t) {
@@ -544,12 +550,15 @@ __device__ __forceinline__ void prompt_part(const SharedArgs &a, const SharedIte
                 to[stage_chunk<BF, Ge::S>(Ge::RPI * (i0 + j) + lane / Ge::S, lane % Ge::S)] = ld[j];
         };
         u32x4s ld[LPT];
-        load(ld, -1);
-        load_queries<BF, D, QT>(a, it, q0, nq, w);
-        put(ld, -1);
-        load(ld, 0);
-        put(ld, 0);
-        load(ld, 1);
+        {  // (the first steps' loads together: one round trip)
+            u32x4s l0[LPT];
+            load(ld, -1);
+            load(l0, 0);
+            load_queries<BF, D, QT>(a, it, q0, nq, w);
+            put(ld, -1);
+            load(ld, 1);
+            put(l0, 0);
+        }
         lds_barrier();
         typename Ge::X x, y;
         first_tile<BF, D, QT>(stage, x, nrows, 0u, a.qscale, w);
@@ -617,15 +626,16 @@ __global__ __launch_bounds__(kShThreads, 2) void k_shared(SharedArgs a)
     typedef ShGeo<BF, D, 16> Ge;
     __shared__ u32x4s lds[kShWaves * 2 * Ge::TILE];
     static_assert(sizeof lds >= kShWaves * (BF ? 32 : 16) * D * sizeof(float), "the stages and the waves' sums share LDS");
-    const int64_t b = (int64_t)blockIdx.z * kGridX + blockIdx.x;
+    const uint32_t b = blockIdx.z * (uint32_t)kGridX + blockIdx.x;
+    const uint32_t prompts = (uint32_t)a.grid.prompt_blocks;
     SharedItem it;
-    if (b < a.grid.prompt_blocks) {
+    if (b < prompts) {
         prompt_item(a, b, it);
         if (it.rows > 0) prompt_part<BF, D, WQ>(a, it, lds);
     } else {
         const int wv = uniform_i32(threadIdx.x >> 6);
-        const int64_t w = (b - a.grid.prompt_blocks) * kShWaves + wv;
-        if (w >= a.grid.tail_waves) return;
+        const uint32_t w = (b - prompts) * kShWaves + wv;
+        if (w >= (uint32_t)a.grid.tail_waves) return;
         tail_item(a, w, it);
         if (it.rows > 0) tail_part<BF, D>(a, it, lds + wv * 2 * Ge::TILE);
     }

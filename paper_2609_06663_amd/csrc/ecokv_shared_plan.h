@@ -38,16 +38,19 @@ __host__ __device__ inline int64_t tail_row(const TailMap &m, int Hkv, int l, in
     return ((((int64_t)l * m.pages + page) * Hkv + h) << m.shift) + (row & ((1 << m.shift) - 1));
 }
 
-// Rows of one of `parts` equal parts of n rows, a multiple of `step`, and how
-// many parts have rows.
-__host__ __device__ inline int64_t part_rows(int n, int parts, int step)
+// Rows of one of `parts` equal parts of n rows, a multiple of `step` (a power of
+// two), and how many parts have rows.  (Unsigned: n plus what rounding adds may
+// pass 2^31, and 32-bit divisions take a third of the time of 64-bit ones.)
+__host__ __device__ inline uint32_t part_rows(int n, int parts, int step)
 {
-    const int64_t r = ((int64_t)n + parts - 1) / parts;
-    return (r + step - 1) / step * step;
+    const uint32_t r = ((uint32_t)n + (uint32_t)parts - 1u) / (uint32_t)parts;
+    return (r + (uint32_t)step - 1u) & ~((uint32_t)step - 1u);
 }
 __host__ __device__ inline int parts_used(int n, int parts, int step)
 {
-    return n > 0 ? (int)((n + part_rows(n, parts, step) - 1) / part_rows(n, parts, step)) : 0;
+    if (n <= 0) return 0;
+    const uint32_t r = part_rows(n, parts, step);
+    return (int)(((uint32_t)n + r - 1u) / r);
 }
 
 // A call's work.

@@ -31,7 +31,7 @@ static int covers(int n, int parts, int step) {
     if (used > parts) return 1;
     if (n <= 0) return used != 0;
     const long long pr = part_rows(n, parts, step);
-    if (pr % step || pr > kShMostRows + step) return 2;
+    if (pr % step || pr > kShMostRows + 2 * step || (step & (step - 1))) return 2;
     for (int p = 0; p < parts; ++p) {
         const long long left = (long long)n - p * pr;
         if ((left > 0) != (p < used)) return 3;
