@@ -648,14 +648,15 @@ struct ShParts {
     int np, nt;
     bool bad;
 };
-__device__ __forceinline__ ShParts row_parts(const SharedArgs &a, int64_t qrow)
+__device__ __forceinline__ ShParts row_parts(const SharedArgs &a, uint32_t qrow)
 {
-    const int c = (int)(qrow % a.N), q = (int)((qrow / a.N) % a.Hq), l = (int)(qrow / ((int64_t)a.N * a.Hq));
+    const uint32_t lq = qrow / (uint32_t)a.N, lh = lq / (uint32_t)a.G;  // (heads of a group are neighbours in every layer)
+    const int c = (int)(qrow - lq * (uint32_t)a.N);
     ShParts r{0, 0, false};
     if (a.max_count > 0) {
         int s = 0;
         while (s + 1 < a.B && a.fan[s + 1] <= c) ++s;
-        const int n = a.counts[((int64_t)l * a.Hkv + q / a.G) * a.B + s];
+        const int n = a.counts[(int64_t)lh * a.B + s];
         r.bad = n < 0 || n > a.max_count;
         r.np = r.bad ? 0 : parts_used(n, a.grid.np, a.grid.step);
     }
@@ -673,26 +674,25 @@ __device__ __forceinline__ bool has_part(const SharedArgs &a, const ShParts &r, 
 }
 
 // O and lse of a query row from its merged (reference, sum) and four sums.
-__device__ __forceinline__ void write_out(const SharedArgs &a, int64_t qrow, int d, bool bad, float M, float L, f32x4s o)
+__device__ __forceinline__ void write_out(const SharedArgs &a, uint32_t qrow, int d, bool bad, float M, float L, f32x4s o)
 {
     // (L is 0 without rows and where every logit is -inf, NaN where one is)
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = bad ? NAN : (L == 0.f ? 0.f : o[e] / L);
-    *reinterpret_cast<f32x4s *>(a.O + qrow * a.D + d) = o;
+    *reinterpret_cast<f32x4s *>(a.O + (int64_t)qrow * a.D + d) = o;
     if (d == 0 && a.lse) a.lse[qrow] = bad ? NAN : (L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f);
 }
 
 // Up to kShFew partials: D / 4 threads per query row, every place of the
 // workspace loaded at once, ahead of the counts that say which hold a partial
 // (the others' contents are not used).
-constexpr int kShMergeThreads = 256, kShFew = 16;
+constexpr int kShMergeThreads = 256, kShFew = 24;
 template <int D, int FEW>
 __global__ __launch_bounds__(kShMergeThreads) void k_shared_merge_few(SharedArgs a)
 {
     constexpr int ROWS = kShMergeThreads / (D / 4);
-    const int64_t block = (int64_t)blockIdx.z * kGridX + blockIdx.x;
-    const int64_t qrow = block * ROWS + threadIdx.x / (D / 4);
-    if (qrow >= a.grid.qrows) return;
+    const uint32_t qrow = (blockIdx.z * (uint32_t)kGridX + blockIdx.x) * ROWS + threadIdx.x / (D / 4);
+    if (qrow >= (uint32_t)a.grid.qrows) return;
     const int d = 4 * (threadIdx.x % (D / 4)), P = a.grid.np + a.grid.nt;
     f32x4s v[FEW];
     float2 e[FEW];
@@ -727,8 +727,8 @@ __global__ __launch_bounds__(kShMergeThreads) void k_shared_merge(SharedArgs a)
     constexpr int GROUPS = kShMergeThreads / (D / 4), REGS = 8;
     __shared__ float wt[kShMergeThreads], red[2][kShMergeThreads / kWave];
     __shared__ f32x4s osum[GROUPS][D / 4];
-    const int64_t qrow = (int64_t)blockIdx.z * kGridX + blockIdx.x;
-    if (qrow >= a.grid.qrows) return;
+    const uint32_t qrow = blockIdx.z * (uint32_t)kGridX + blockIdx.x;
+    if (qrow >= (uint32_t)a.grid.qrows) return;
     const int t = threadIdx.x, lane = t & 63, wv = t >> 6, P = a.grid.np + a.grid.nt;
     const int d = 4 * (t % (D / 4)), grp = t / (D / 4);
     const ShParts r = row_parts(a, qrow);
@@ -793,8 +793,11 @@ template <int D>
 static void launch_merge(const SharedArgs &a, int few, dim3 grid, hipStream_t st)
 {
     const dim3 b(kShMergeThreads);
-    if (few == 4) hipLaunchKernelGGL((k_shared_merge_few<D, 4>), grid, b, 0, st, a);
+    if (few == 2) hipLaunchKernelGGL((k_shared_merge_few<D, 2>), grid, b, 0, st, a);
+    else if (few == 3) hipLaunchKernelGGL((k_shared_merge_few<D, 3>), grid, b, 0, st, a);
+    else if (few == 5) hipLaunchKernelGGL((k_shared_merge_few<D, 5>), grid, b, 0, st, a);
     else if (few == 8) hipLaunchKernelGGL((k_shared_merge_few<D, 8>), grid, b, 0, st, a);
+    else if (few == 14) hipLaunchKernelGGL((k_shared_merge_few<D, 14>), grid, b, 0, st, a);
     else if (few == kShFew) hipLaunchKernelGGL((k_shared_merge_few<D, kShFew>), grid, b, 0, st, a);
     else hipLaunchKernelGGL(k_shared_merge<D>, grid, b, 0, st, a);
 }
@@ -815,7 +818,7 @@ hipError_t shared_launch(SharedArgs a, bool bf16, hipStream_t st)
         if (e != hipSuccess) return e;
     }
     const int parts = a.grid.np + a.grid.nt;
-    const int few = parts <= 4 ? 4 : parts <= 8 ? 8 : parts <= kShFew ? kShFew : 0;
+    const int few = parts <= 2 ? 2 : parts <= 3 ? 3 : parts <= 5 ? 5 : parts <= 8 ? 8 : parts <= 14 ? 14 : parts <= kShFew ? kShFew : 0;
     const int per = few ? kShMergeThreads / (a.D / 4) : 1;
     const dim3 g = grid((a.grid.qrows + per - 1) / per);
     ECOKV_TIMED("shared_merge", st, (a.D == 128 ? launch_merge<128>(a, few, g, st) : launch_merge<64>(a, few, g, st)));
