@@ -1107,7 +1107,7 @@ int ecokv_decode_shared(const void *Q_dec, const void *Kc, const void *Vc, int d
                                 dtype == ECOKV_BF16);
     if (a.grid.prompt_blocks > INT32_MAX - (1 << 20) || a.grid.tail_waves > INT32_MAX - (1 << 20))
         return fail(ECOKV_EINVAL, "too many parts of kept rows or tails");
-    if (!workspace) return fail(ECOKV_EINVAL, "workspace is NULL");
+    if (!workspace && a.grid.bytes > 0) return fail(ECOKV_EINVAL, "workspace is NULL");
     if (((uintptr_t)workspace & 255u) != 0) return fail(ECOKV_EINVAL, "workspace must be 256-byte aligned");
     if (workspace_bytes < a.grid.bytes)
         return fail(ECOKV_EWORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, a.grid.bytes);

@@ -695,7 +695,8 @@ __device__ __forceinline__ void write_out(const SharedArgs &a, uint32_t qrow, in
 
 // Up to kShFew partials: D / 4 threads per query row, every place of the
 // workspace loaded at once, ahead of the counts that say which hold a partial
-// (the others' contents are not used).
+// (the others' contents are not used).  A call without kept rows and tails has
+// no places.
 constexpr int kShMergeThreads = 256, kShFew = 24;
 template <int D, int FEW>
 __global__ __launch_bounds__(kShMergeThreads) void k_shared_merge_few(SharedArgs a)
@@ -704,6 +705,10 @@ __global__ __launch_bounds__(kShMergeThreads) void k_shared_merge_few(SharedArgs
     const uint32_t qrow = (blockIdx.z * (uint32_t)kGridX + blockIdx.x) * ROWS + threadIdx.x / (D / 4);
     if (qrow >= (uint32_t)a.grid.qrows) return;
     const int d = 4 * (threadIdx.x % (D / 4)), P = a.grid.np + a.grid.nt;
+    if (P == 0) {
+        write_out(a, qrow, d, false, -INFINITY, 0.f, (f32x4s){});
+        return;
+    }
     f32x4s v[FEW];
     float2 e[FEW];
 #pragma unroll

@@ -155,6 +155,20 @@ def test_prompt_alone_and_tail_alone(dtype, D):
     c.check(O1, lse1)
 
 
+@pytest.mark.parametrize("dtype,D,N", [("bf16", 128, 5), ("f32", 64, 1)])
+def test_neither_prompts_nor_tails(dtype, D, N):
+    # both bounds 0: the workspace has no places, and none may be read
+    import paper_2609_06663_amd as P
+    c = Case(19, dtype, 1, 8, 2, D, [[[0], [0]]], [N], [0] * N, 16)
+    say(f"{dtype} D={D}: no rows at all")
+    assert P.ecokv_decode_shared_workspace_size(c.shape, c.fan, 0, 0) == 0
+    for ws in (None, torch.empty(0, dtype=torch.uint8, device="cuda")):
+        O, lse = torch.full((1, 8, N, D), -7.0, device="cuda"), torch.full((1, 8, N), -7.0, device="cuda")
+        P.ecokv_decode_shared(c.Q, None, None, c.shape, c.fan, None, None, 0, None, None, 0, O, lse, ws)
+        torch.cuda.synchronize()
+        assert bool((O == 0).all()) and bool((lse == -float("inf")).all())
+
+
 def test_one_continuation_each_is_plain_decode():
     import paper_2609_06663_amd as P
     c = Case(9, "bf16", 2, 28, 4, 128, [[[900, 64, 2000]] * 4] * 2, [1, 1, 1], [0, 0, 0], 16)
