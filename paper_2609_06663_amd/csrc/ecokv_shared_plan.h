@@ -11,7 +11,7 @@
 namespace ecokv {
 
 constexpr int kShWaves = 4;                     // waves per block
-constexpr int kShNarrow = 50 << 20;
+constexpr int kShNarrow = 50 << 20;             // bytes (see shared_grid)
 constexpr int kTailQ = 16;                      // query heads of a wave in the tails
 // Blocks (and four times as many waves of the tails) that the parts may make: one
 // per compute unit.  Two fit, but every further part is a partial of each query
@@ -100,9 +100,9 @@ inline SharedGrid shared_grid(int64_t pairs, int G, int D, int B, const int32_t 
     // As many waves along the query rows as the largest prompt fills: each row of
     // the cache then serves them all from LDS.  But where the tiles of rows_q
     // together read no more than kShNarrow bytes, a block for each: the L2s bear
-    // that, and no wave of a small prompt idles (us, wide and narrow: five prompts,
-    // 48 MB, 27.7 and 25.5; 14 tiles of 1000 rows, 29 MB, 23.1 and 17.0; 4 of 6553
-    // rows, 54 MB, 21.8 and 24.0; 16 layers' worth of those, 752 MB, 74 and 121).
+    // that, and more blocks share the rows' latency (us, wide and narrow: 14 tiles
+    // of 1000 rows of 4 heads, 29 MB, 23.1 and 17.0; 4 of 6553 rows, 54 MB, 21.8 and
+    // 24.0; 14 layers of those, 752 MB, 74 and 121).
     const bool narrow = (double)(pairs * tiles) * max_count * D * (bf16 ? 4 : 8) <= (double)kShNarrow;
     g.wq = narrow ? 1 : most > 2 * g.rows_q ? 4 : most > g.rows_q ? 2 : 1;
     g.step = g.rows_t * (kShWaves / g.wq);

@@ -149,3 +149,75 @@ class LayerwiseEviction:
         wait between blocks give up (see ecokv_workspace_status)."""
         for s, ws in zip(self.streams, self.workspaces):
             E.ecokv_workspace_status(ws, s)
+
+
+class Continuations:
+    """Generation from the compressed prompts of an `EvictionPass`.
+
+    Prompt s is continued by fan_out[s] continuations of up to `max_new` tokens
+    each, whose keys and values lie in paged tails; all continuations of a
+    prompt share its kept rows.  For every generated token, `step` takes the new
+    queries, keys and values as the projections wrote them ([L][N][heads][D],
+    views of a fused tensor will do), norms and rotates queries and keys (`rope`),
+    appends keys and values and attends: O [L][H_q][N][D] float32 and lse; then
+    `advance` moves on.  Positions go on from the prompts' own lengths, whatever
+    was evicted.  The pass may hold one layer or several; with a pass per layer,
+    each layer has its own instance, advanced with the others.
+
+    `step` and `advance` only enqueue work, on one stream at a time (they share a
+    workspace).  To capture them in a HIP graph, pass `step` max_tail=max_new: by
+    default it is the present length, which a replay would not raise.  A replay
+    moves the device's counters only; `length` is the caller's to keep."""
+
+    def __init__(self, ep: EvictionPass, fan_out, max_new: int, rope: E.Rope, page_size: int = 64):
+        shape = ep.shape
+        c = shape.c
+        fan_out = E._flat_ints(fan_out)
+        if len(fan_out) != c.num_seqs or min(fan_out) < 0:
+            raise ValueError("fan_out has the number of continuations of each prompt")
+        if sum(fan_out) < 1:
+            raise ValueError("fan_out has no continuation")
+        if max_new < 1:
+            raise ValueError(f"max_new {max_new} < 1")
+        self.ep, self.rope, self.max_new, self.length = ep, rope, int(max_new), 0
+        self.fan = [0]
+        for f in fan_out:
+            self.fan.append(self.fan[-1] + f)
+        N, L, Hq, Hkv, D = self.fan[-1], c.num_layers, c.num_q_heads, c.num_kv_heads, c.head_dim
+        dev, dtype = ep.Kc.device, ep.Kc.dtype
+        per = -(-self.max_new // page_size)
+        self.tails = E.Tails(*(torch.empty((L, N * per, Hkv, page_size, D), dtype=dtype, device=dev) for _ in range(2)),
+                             torch.arange(N * per, dtype=torch.int32, device=dev).view(N, per))
+        cu = shape.cu_seqlens
+        start = [cu[s + 1] - cu[s] for s in range(c.num_seqs) for _ in range(fan_out[s])]
+        # row of the next token, rows with it, its position
+        self._at = torch.tensor([[0] * N, [1] * N, start], dtype=torch.int32, device=dev)
+        self.rows, self.tail_counts, self.positions = self._at
+        # rows that one head can keep: the budget, or what the heads of a layer share
+        w, lens = c.window, [cu[s + 1] - cu[s] for s in range(c.num_seqs)]
+        if ep.mode == E.LAYER_FLAT:
+            self.max_count = max(min(t, Hkv * (b - w) + w) for t, b in zip(lens, ep.budget))
+        elif ep.mode == E.HEAD_BUDGETS:
+            self.max_count = min(max(lens), max(ep.budget))
+        else:
+            self.max_count = max(min(t, b) for t, b in zip(lens, ep.budget))
+        self.Q_dec = torch.empty((L, Hq, N, D), dtype=dtype, device=dev)
+        self.O = torch.empty((L, Hq, N, D), dtype=torch.float32, device=dev)
+        self.lse = torch.empty((L, Hq, N), dtype=torch.float32, device=dev)
+        self.workspace = torch.empty(
+            max(E.ecokv_decode_shared_workspace_size(shape, self.fan, self.max_count, self.max_new), 256), dtype=torch.uint8, device=dev)
+
+    def step(self, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, stream=None, max_tail: Optional[int] = None) -> torch.Tensor:
+        """Append the next token of every continuation and attend; returns O."""
+        if self.length >= self.max_new:
+            raise ValueError(f"the tails hold {self.max_new} tokens")
+        E.ecokv_append(Q, K, V, self.ep.shape, self.rope, self.positions, None, self.rows, self.tails, self.Q_dec, stream)
+        E.ecokv_decode_shared(self.Q_dec, self.ep.Kc, self.ep.Vc, self.ep.shape, self.fan, self.ep.counts, self.ep.offsets, self.max_count,
+                              self.tails, self.tail_counts, self.length + 1 if max_tail is None else max_tail, self.O, self.lse,
+                              self.workspace, stream)
+        return self.O
+
+    def advance(self) -> None:
+        """On to the next token (enqueued on the current stream)."""
+        self._at.add_(1)
+        self.length += 1
