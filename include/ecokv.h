@@ -389,7 +389,8 @@ int ecokv_decode(const void *Q_dec, const void *Kc, const void *Vc, int dtype, c
  *   dimensions rot_dim .. D-1 stay.
  * Pair i is (i, i + rot_dim / 2), or (2 i, 2 i + 1) if interleaved.  Norms,
  * angles (p freq[i] and its reduction in 64 bits) and turns are computed in
- * 32 bits or more and rounded to the element type once, at the end. */
+ * 32 bits or more and rounded to the element type once, at the end (so where a
+ * row is normed, mean(x^2) + norm_eps is to be a normal number of 32 bits). */
 typedef struct ecokv_rope {
     int32_t rot_dim;      /* dimensions rotated: a multiple of 16 in [0, D]        */
     int32_t interleaved;  /* 0 or 1                                               */
@@ -397,8 +398,8 @@ typedef struct ecokv_rope {
                           /* NULL if rot_dim is 0 (see ecokv_rope_freqs)          */
     float factor;         /* of cosines and sines; 1 for unscaled rotary positions */
     float norm_eps;       /* >= 0                                                 */
-    const void *q_norm;   /* DEVICE [D] weights of the element type, or NULL      */
-    const void *k_norm;
+    const void *q_norm;   /* DEVICE [D] weights of the element type, 16-byte      */
+    const void *k_norm;   /* aligned, or NULL                                     */
 } ecokv_rope;
 
 /* How ecokv_rope_freqs changes the frequencies base^(-2i/rot_dim) for contexts
@@ -503,8 +504,11 @@ int ecokv_decode_shared_workspace_size(const ecokv_shape *shape, const int32_t *
  * the attended rows, give NaN outputs for the continuations concerned.
  * Arithmetic: fp32 accumulation (bf16 rows: the weights as three bf16 summands
  * each, 24 bits, so a value row with an infinity gives NaN).
- * Q_dec, Kc, Vc and the tails' K and V must be 16-byte aligned, the workspace
- * 256-byte aligned; it needs no initial contents. */
+ * Q_dec, Kc, Vc, O and the tails' K and V must be 16-byte aligned, the workspace
+ * 256-byte aligned; it needs no initial contents (none at all if both bounds are
+ * 0), and belongs to one call at a time: calls and graph replays that share one
+ * must be ordered.  Results do not depend on what else runs: the same call gives
+ * the same bits. */
 int ecokv_decode_shared(const void *Q_dec, const void *Kc, const void *Vc, int dtype, const ecokv_shape *shape,
                         const int32_t *fan, const int32_t *counts, const int32_t *offsets, int32_t max_count,
                         const ecokv_tails *tails, const int32_t *tail_counts, int32_t max_tail, float *O, float *lse,

@@ -880,6 +880,8 @@ int check_rope(const ecokv_rope *r, int D)
     if (r->rot_dim > 0 && !r->freq) return fail(ECOKV_EINVAL, "freq is NULL");
     if (!isfinite(r->factor)) return fail(ECOKV_EINVAL, "factor %g", (double)r->factor);
     if (!(isfinite(r->norm_eps) && r->norm_eps >= 0.f)) return fail(ECOKV_EINVAL, "norm_eps %g", (double)r->norm_eps);
+    if ((((uintptr_t)r->q_norm | (uintptr_t)r->k_norm) & 15u) != 0)
+        return fail(ECOKV_EINVAL, "q_norm and k_norm must be 16-byte aligned");
     return ECOKV_OK;
 }
 
@@ -888,6 +890,7 @@ int check_rope(const ecokv_rope *r, int D)
 int check_rows(const void *p, int64_t stride, int64_t tokens, int64_t elems, int es, const char *name, Span *span)
 {
     if (((uintptr_t)p & 15u) != 0) return fail(ECOKV_EINVAL, "%s must be 16-byte aligned", name);
+    if (elems > INT32_MAX / 8) return fail(ECOKV_EINVAL, "a token of %s has %lld elements", name, (long long)elems);
     if (stride < elems || stride * es % 16 != 0 || stride > INT64_MAX / 4 / (tokens > 0 ? tokens : 1) / es)
         return fail(ECOKV_EINVAL, "the stride %lld of %s is below a token's %lld elements or no multiple of 16 bytes",
                     (long long)stride, name, (long long)elems);
@@ -1091,8 +1094,8 @@ int ecokv_decode_shared(const void *Q_dec, const void *Kc, const void *Vc, int d
     if (!Q_dec || !O) return fail(ECOKV_EINVAL, "Q_dec and O must be non-NULL");
     if (max_count > 0 && (!Kc || !Vc || !counts || !offsets))
         return fail(ECOKV_EINVAL, "Kc, Vc, counts and offsets must be non-NULL");
-    if ((((uintptr_t)Q_dec | (uintptr_t)Kc | (uintptr_t)Vc) & 15u) != 0)
-        return fail(ECOKV_EINVAL, "Q_dec, Kc and Vc must be 16-byte aligned");
+    if ((((uintptr_t)Q_dec | (uintptr_t)Kc | (uintptr_t)Vc | (uintptr_t)O) & 15u) != 0)
+        return fail(ECOKV_EINVAL, "Q_dec, Kc, Vc and O must be 16-byte aligned");
     if (max_tail > 0) {
         Span tk, tv;
         if ((rc = check_tails(tails, si, dtype == ECOKV_BF16 ? 2 : 4, &a.map, &tk, &tv))) return rc;

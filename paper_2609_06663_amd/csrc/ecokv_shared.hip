@@ -490,9 +490,9 @@ __device__ __forceinline__ void prompt_part(const SharedArgs &a, const SharedIte
     const int q0 = it.q0 + wq * QT, nq = min(it.nq - wq * QT, QT);
     const int64_t base = (it.base + it.row0 + first) * Ge::RB;
     const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<char *>(uniform_ptr(a.Kc + base)), (short)0, uniform_i32(nrows * Ge::RB), 0x00020000);
+        const_cast<char *>(uniform_ptr(a.Kc + base)), (short)0, uniform_i32((int)((uint32_t)nrows * Ge::RB)), 0x00020000);
     const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<char *>(uniform_ptr(a.Vc + base)), (short)0, uniform_i32(nrows * Ge::RB), 0x00020000);
+        const_cast<char *>(uniform_ptr(a.Vc + base)), (short)0, uniform_i32((int)((uint32_t)nrows * Ge::RB)), 0x00020000);
     u32x4s *const stage = lds + kgi * (WQ > 1 ? 4 : 2) * Ge::TILE;
     ShState<BF, D, QT> w;
     if constexpr (WQ == 1) {
@@ -503,7 +503,7 @@ __device__ __forceinline__ void prompt_part(const SharedArgs &a, const SharedIte
 #pragma unroll
             for (int i = 0; i < Ge::NL; ++i)
                 x[i] = __builtin_bit_cast(u32x4s, __builtin_amdgcn_raw_buffer_load_b128(
-                    rs, (t * Ge::TR + Ge::RPI * i) * Ge::RB + lane * 16, 0, 0));
+                    rs, (int)((uint32_t)(t * Ge::TR + Ge::RPI * i) * Ge::RB + lane * 16), 0, 0));
         };
         const auto put = [&](const u32x4s (&x)[Ge::NL], u32x4s *to) {
 #pragma unroll
@@ -540,7 +540,7 @@ __device__ __forceinline__ void prompt_part(const SharedArgs &a, const SharedIte
 #pragma unroll
             for (int j = 0; j < LPT; ++j)
                 ld[j] = __builtin_bit_cast(u32x4s, __builtin_amdgcn_raw_buffer_load_b128(
-                    rs, ((s + (isk ? 1 : 0)) * Ge::TR + Ge::RPI * (i0 + j)) * Ge::RB + lane * 16, 0, 0));
+                    rs, (int)((uint32_t)((s + (isk ? 1 : 0)) * Ge::TR + Ge::RPI * (i0 + j)) * Ge::RB + lane * 16), 0, 0));
         };
         // K tiles at stage + (tile & 1) TILE, V tiles two TILEs on
         const auto put = [&](const u32x4s (&ld)[LPT], int s) {

@@ -70,7 +70,7 @@ def rope(E, **kw):
 
 BAD_ROPES = [(dict(rot_dim=-16), -1), (dict(rot_dim=130), -1), (dict(rot_dim=144), -1), (dict(rot_dim=17), -1), (dict(rot_dim=24), -3), (dict(rot_dim=2), -3),
              (dict(interleaved=2), -1), (dict(freq=None), -1), (dict(factor=float("nan")), -1), (dict(factor=float("inf")), -1),
-             (dict(norm_eps=-1.0), -1), (dict(norm_eps=float("nan")), -1)]
+             (dict(norm_eps=-1.0), -1), (dict(norm_eps=float("nan")), -1), (dict(q_norm=ctypes.c_void_p(264)), -1), (dict(k_norm=ctypes.c_void_p(264)), -1)]
 
 
 def test_prefill_rope_refusals(P, E):
@@ -100,6 +100,7 @@ def test_prefill_rope_refusals(P, E):
     assert call(Qo=at(4)) == -1 and call(win=at(3)) == -1 and call(win=at(4)) == -1 and call(Ko=at(0)) == -1 and call(win=at(0)) == -1
     assert "overlap" in P.ecokv_last_error()
     assert call(qs=1 << 62) == -1
+    assert call(shape=P.Shape(1, 1 << 24, 1, 128, 4, [0, 9]), qs=1 << 31, ks=128) == -1   # a token of 2^31 elements
     assert f(None, 0, None, 0, 0, ctypes.byref(P.Shape(0, 8, 2, 128, 4, [0, 9]).c), ctypes.byref(rope(E)), None, None, None, None, None) == 0
     assert f(None, 0, None, 0, 0, ctypes.byref(s.c), ctypes.byref(rope(E)), None, None, None, None, None) == 0   # nothing asked for
     assert f(None, 0, None, 0, 0, ctypes.byref(s.c), None, None, None, None, None, None) == -1
@@ -164,7 +165,7 @@ def test_decode_shared_refusals(P, E):
     assert call(t=good, fn=None) == -1 and call(t=good, fn=fan(0, 3, 2)) == -1
     for m in ("Q", "Kc", "Vc", "cnt", "off", "O", "tc"):
         assert call(t=good, **{m: None}) == -1, m
-    for m in ("Q", "Kc", "Vc"):
+    for m in ("Q", "Kc", "Vc", "O"):
         assert call(t=good, **{m: ctypes.c_void_p(264)}) == -1, m
     assert call(t=good, dtype=3) == -3
     assert call(t=good, shape=P.Shape(2, 8, 2, 32, 4, [0, 100, 250])) == -3
