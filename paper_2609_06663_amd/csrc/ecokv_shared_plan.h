@@ -11,12 +11,12 @@
 namespace ecokv {
 
 constexpr int kShWaves = 4;                     // waves per block
-constexpr int kShNarrow = 50 << 20;             // bytes (see shared_grid)
+constexpr int kShNarrow = 210 << 20;            // bytes (see shared_grid)
 constexpr int kTailQ = 16;                      // query heads of a wave in the tails
 // Blocks (and four times as many waves of the tails) that the parts may make: one
 // per compute unit.  Two fit, but every further part is a partial of each query
 // row to write and to merge (us, 256 against 512: 64 continuations of 6553 rows
-// 45 and 55, 20 of 64 heads of 8191 rows 41 and 44; 28 layers of 16 139 and 136).
+// 40 and 49, 20 of 64 heads of 8191 rows 39 and 43; 28 layers of 16 139 and 134).
 constexpr int kShBlocks = 256;
 constexpr int kShMostRows = 1 << 22;            // rows of a part at most: its bytes are addressed by 32 bits
 
@@ -99,10 +99,12 @@ inline SharedGrid shared_grid(int64_t pairs, int G, int D, int B, const int32_t 
     }
     // As many waves along the query rows as the largest prompt fills: each row of
     // the cache then serves them all from LDS.  But where the tiles of rows_q
-    // together read no more than kShNarrow bytes, a block for each: the L2s bear
-    // that, and more blocks share the rows' latency (us, wide and narrow: 14 tiles
-    // of 1000 rows of 4 heads, 29 MB, 23.1 and 17.0; 4 of 6553 rows, 54 MB, 21.8 and
-    // 24.0; 14 layers of those, 752 MB, 74 and 121).
+    // together read no more than kShNarrow bytes, a block for each: the L2 of the
+    // XCD that has all of a part's tiles bears that, more blocks share the rows'
+    // latency, and no wave of a small prompt idles (us, wide and narrow: 14 tiles of
+    // 6553 rows of 4 heads, 188 MB, 31.1 and 25.0; 4 layers of 4 such tiles, 215 MB,
+    // 29.1 and 26.2; 4 tiles of 30000 rows, 246 MB, 28.5 and 31.2; 14 layers of 4
+    // tiles of 6553, 752 MB, 59 and 67; fp32, 8 tiles of 6553, 215 MB, 29.3 and 29.5).
     const bool narrow = (double)(pairs * tiles) * max_count * D * (bf16 ? 4 : 8) <= (double)kShNarrow;
     g.wq = narrow ? 1 : most > 2 * g.rows_q ? 4 : most > g.rows_q ? 2 : 1;
     g.step = g.rows_t * (kShWaves / g.wq);

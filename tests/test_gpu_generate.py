@@ -184,6 +184,7 @@ def test_graph_replays_of_prompts_and_of_large_splits():
     from test_gpu_shared import Case
     m = Model(3, "bf16", 1, 28, 4, 128, 4, [2000])
     c = Case(18, "bf16", 1, 28, 4, 128, [[[6553]] * 4], [20], [100 + 9 * i for i in range(20)], 16)
+    c.max_count = 3_000_000
     L, Hq, Hkv, D, w = m.dims
     e = lambda *s, dtype=torch.bfloat16: torch.empty(s, dtype=dtype, device="cuda")
     Q, K, V = (t.contiguous() for t in m.project(2000))

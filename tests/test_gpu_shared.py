@@ -137,6 +137,39 @@ def test_shared(case, kscale):
     assert torch.equal(O, O3) and torch.equal(lse, lse3)
 
 
+@pytest.mark.parametrize("case", SHAPES, ids=lambda c: f"{c[0]}-D{c[1]}-L{c[2]}-{c[3]}q{c[4]}kv-{c[5]}-{c[6]}-p{c[8]}")
+def test_shared_as_in_large_calls(case):
+    # a bound of 3 million kept rows: split like a call that reads gigabytes, with
+    # blocks of as many query rows as the largest prompt fills
+    dtype, D, L, Hq, Hkv, counts, fan, tails, page = case
+    say(f"{case[:7]} page {page}, split for 3 million rows")
+    c = Case(20, dtype, L, Hq, Hkv, D, [[counts] * Hkv] * L, fan, tails, page)
+    O, lse = c.run(max_count=3_000_000)
+    c.check(O, lse)
+    O2, lse2 = c.run(max_count=3_000_000)
+    assert torch.equal(O, O2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+def test_rows_of_weight_zero_in_large_calls(dtype, D):
+    # the same with dead rows at a part's ends, and NaN in one unit
+    c = Case(21, dtype, 1, 8, 2, D, [[[1400], [600]]], [20], [50, 0] * 10, 16)
+    c.Q[..., 0] = 1.0
+    c.Kc[:300, 0] = -float("inf")
+    c.Kc[1350:1400, 0] = -float("inf")
+    c.Kc[1700, 3] = float("nan")
+    say(f"{dtype} D={D}: rows of weight zero, split for 3 million rows")
+    O, lse = c.run(max_count=3_000_000)
+    assert bool(O[:, 4:].isnan().all()) and bool(lse[:, 4:].isnan().all())
+    for k in range(20):
+        K, V = (x.double() for x in c.rows_of(0, 0, k))
+        q = c.Q[0, :4, k].double()
+        dead = K[:, 0] == -float("inf")
+        x = (q @ K.masked_fill(dead[:, None], 0).t() / D ** 0.5).masked_fill(dead, -float("inf"))
+        assert float((O[0, :4, k].double() - x.softmax(1) @ V).abs().max()) <= 1e-4 * float(V.abs().max()), k
+        assert bool(((lse[0, :4, k].double() - x.logsumexp(1)).abs() <= 1e-4).all()), k
+
+
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
 def test_prompt_alone_and_tail_alone(dtype, D):
     c = Case(8, dtype, 1, 14, 2, D, [[[333, 129], [400, 1]]], [3, 2], [40, 1, 77, 0, 16], 16)
