@@ -62,15 +62,18 @@ __device__ __forceinline__ u32x4r pack_row(const float (&f)[BF ? 8 : 4])
     return x;
 }
 
-// cos and sin of p w.  The angle is p w in turns, reduced to [-1/2, 1/2] in 64
-// bits (the product of a 31-bit position and a 24-bit frequency needs more than
-// 32 bits to keep its fraction), the rest in 32.
+// cos and sin of p w.  The angle is p w in turns, reduced to an eighth of one
+// beside a quarter in 64 bits (the product of a 31-bit position and a 24-bit
+// frequency needs more than 32 bits to keep its fraction; an eighth rounds to 32
+// with 2.3e-8 radians at most, half a turn with 9.4e-8), the rest in 32.
 __device__ __forceinline__ float2 turn(int p, float w, float factor)
 {
-    const double t = (double)p * (double)w * 0.15915494309189533577;
+    const double t = 4.0 * ((double)p * (double)w * 0.15915494309189533577), n = rint(t);
+    const int q = (int)(n - 4.0 * floor(0.25 * n));  // quarters, 0 .. 3
     float s, c;
-    sincospif(2.f * (float)(t - rint(t)), &s, &c);
-    return make_float2(factor * c, factor * s);
+    sincospif(0.5f * (float)(t - n), &s, &c);
+    const float cq = q & 1 ? -s : c, sq = q & 1 ? c : s;
+    return q & 2 ? make_float2(-factor * cq, -factor * sq) : make_float2(factor * cq, factor * sq);
 }
 
 // The sequence of packed token t.
