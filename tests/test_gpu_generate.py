@@ -249,3 +249,40 @@ def test_calls_on_several_streams_at_once():
     torch.cuda.synchronize()
     for i, O, lse in outs:
         assert torch.equal(O, want[i][0]) and torch.equal(lse, want[i][1]), i
+
+
+def test_two_graphs_share_a_workspace():
+    # graphs of different splits over one workspace, replayed in order on one
+    # stream with an eager call of the same workspace between them
+    import paper_2609_06663_amd as P
+    from test_gpu_shared import Case
+    cases = [Case(40, "bf16", 1, 28, 4, 128, [[[6553]] * 4], [8], [200] * 8, 64),
+             Case(41, "f32", 1, 8, 2, 64, [[[300, 77]] * 2], [3, 1], [20, 0, 5, 33], 4)]
+    sizes = [P.ecokv_decode_shared_workspace_size(c.shape, c.fan, c.max_count, c.max_tail) for c in cases]
+    ws = torch.empty(max(sizes), dtype=torch.uint8, device="cuda")
+    want = [c.run() for c in cases]
+    outs = [(torch.empty_like(o), torch.empty_like(l)) for o, l in want]
+    tails = [P.Tails(c.tk, c.tv, c.table) for c in cases]
+
+    def work(i):
+        c = cases[i]
+        P.ecokv_decode_shared(c.Q, c.Kc, c.Vc, c.shape, c.fan, c.counts, c.offsets, c.max_count, tails[i], c.tail_counts, c.max_tail, *outs[i], ws)
+
+    graphs = []
+    for i in range(2):
+        work(i)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i]):
+            work(i)
+    for rep in range(4):
+        for o, l in outs:
+            o.zero_(), l.zero_()
+        graphs[rep % 2].replay()
+        work(1 - rep % 2)
+        say(f"round {rep}")
+        torch.cuda.synchronize()
+        graphs[1 - rep % 2].replay()
+        torch.cuda.synchronize()
+        for (o, l), (wo, wl) in zip(outs, want):
+            assert torch.equal(o, wo) and torch.equal(l, wl), rep
