@@ -476,7 +476,9 @@ int ecokv_append(const void *Q_new, int64_t q_stride, const void *K_new, int64_t
                  const int32_t *positions, const int32_t *conts, const int32_t *rows, int32_t num_tokens,
                  const ecokv_tails *tails, void *Q_dec, void *stream);
 
-/* Workspace bytes of ecokv_decode_shared for this shape, fan and these bounds. */
+/* Workspace bytes of ecokv_decode_shared for this shape, fan and these bounds.
+ * Smaller bounds may split the rows otherwise and need more; max_tail alone
+ * never does. */
 int ecokv_decode_shared_workspace_size(const ecokv_shape *shape, const int32_t *fan, int32_t max_count,
                                        int32_t max_tail, size_t *bytes);
 

@@ -116,6 +116,6 @@ def test_parts_cover_every_row_once(lib, G):
                 for bf16 in (0, 1):
                     rc = lib.plan(pairs, G, 128, len(fan), cum.ctypes.data, mc, mt, bf16, n.ctypes.data, len(n), out.ctypes.data)
                     assert rc == 0, (rc, pairs, G, fan, mc, mt, bf16, out.tolist())
-                    # one round of the device, or one part each (of what 32-bit offsets reach)
-                    assert out[2] <= 256 or out[0] == max(1, -(-mc // 2 ** 22))
-                    assert out[3] <= 1024 or out[1] == max(1, -(-mt // 2 ** 22))
+                    # one round of the device, or a few parts each (and those that 32-bit offsets reach)
+                    assert out[2] <= 256 or out[0] <= max(8, -(-mc // 2 ** 22))
+                    assert out[3] <= 2048 or out[1] == max(1, -(-mt // 2 ** 22))
