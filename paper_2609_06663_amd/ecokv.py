@@ -276,15 +276,13 @@ _U8 = (torch.uint8,)
 
 
 def _workspace(workspace: Optional[torch.Tensor], nbytes: int, device, stream):
-    """The caller's workspace, or a zero-filled one allocated here; a tensor
-    allocated here is recorded on `stream`, so that torch's allocator does not
-    hand its memory out again before the work queued there has used it."""
+    """The caller's workspace, or a zero-filled one allocated here, on `stream`
+    where one is given: its memory's last use, the filling and torch's next use
+    are then all in order with the call."""
     if workspace is not None:
         return workspace
-    ws = torch.zeros(max(nbytes, 256), dtype=torch.uint8, device=device)
-    if stream is not None:
-        ws.record_stream(stream)
-    return ws
+    with torch.cuda.stream(stream):  # (None: the current stream stays)
+        return torch.zeros(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
 def _dtype_code(t: torch.Tensor) -> int:

@@ -286,3 +286,26 @@ def test_two_graphs_share_a_workspace():
         torch.cuda.synchronize()
         for (o, l), (wo, wl) in zip(outs, want):
             assert torch.equal(o, wo) and torch.equal(l, wl), rep
+
+
+def test_a_workspace_made_by_the_binding_is_in_order_with_its_stream(monkeypatch):
+    # allocated and filled on the call's stream, whatever the current one is
+    import paper_2609_06663_amd as P
+    from paper_2609_06663_amd import ecokv as E
+    from test_gpu_shared import Case
+    c = Case(50, "bf16", 1, 8, 2, 128, [[[900], [400]]], [3], [20, 0, 5], 16)
+    O, lse = c.run()
+    seen, zeros = [], torch.zeros
+    monkeypatch.setattr(E.torch, "zeros", lambda *a, **k: (seen.append(torch.cuda.current_stream()), zeros(*a, **k))[1])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    O2, lse2 = torch.empty_like(O), torch.empty_like(lse)
+    tails = P.Tails(c.tk, c.tv, c.table)
+    call = lambda **kw: P.ecokv_decode_shared(c.Q, c.Kc, c.Vc, c.shape, c.fan, c.counts, c.offsets, c.max_count, tails, c.tail_counts, c.max_tail,
+                                              O2, lse2, **kw)
+    call(stream=s)
+    s.synchronize()
+    assert torch.equal(O, O2) and torch.equal(lse, lse2)
+    call()
+    torch.cuda.synchronize()
+    assert seen == [s, torch.cuda.current_stream()]
