@@ -165,7 +165,9 @@ class Continuations:
     each layer has its own instance, advanced with the others.
 
     `step` and `advance` only enqueue work, on one stream at a time (they share a
-    workspace).  To capture them in a HIP graph, pass `step` max_tail=max_new: by
+    workspace): `advance` goes where the last `step` went, to the stream that it
+    was given or else to the current one.  Who changes the stream between calls
+    orders the one after the other.  To capture them in a HIP graph, pass `step` max_tail=max_new: by
     default it is the present length, which a replay would not raise.  A replay
     moves the device's counters only; `length` is the caller's to keep."""
 
@@ -180,6 +182,7 @@ class Continuations:
         if max_new < 1:
             raise ValueError(f"max_new {max_new} < 1")
         self.ep, self.rope, self.max_new, self.length = ep, rope, int(max_new), 0
+        self._stream = None  # that the last step was given
         self.fan = [0]
         for f in fan_out:
             self.fan.append(self.fan[-1] + f)
@@ -211,13 +214,15 @@ class Continuations:
         """Append the next token of every continuation and attend; returns O."""
         if self.length >= self.max_new:
             raise ValueError(f"the tails hold {self.max_new} tokens")
+        self._stream = stream
         E.ecokv_append(Q, K, V, self.ep.shape, self.rope, self.positions, None, self.rows, self.tails, self.Q_dec, stream)
         E.ecokv_decode_shared(self.Q_dec, self.ep.Kc, self.ep.Vc, self.ep.shape, self.fan, self.ep.counts, self.ep.offsets, self.max_count,
                               self.tails, self.tail_counts, self.length + 1 if max_tail is None else max_tail, self.O, self.lse,
                               self.workspace, stream)
         return self.O
 
-    def advance(self) -> None:
-        """On to the next token (enqueued on the current stream)."""
-        self._at.add_(1)
+    def advance(self, stream=None) -> None:
+        """On to the next token (enqueued on `stream`, or else on the last step's)."""
+        with torch.cuda.stream(self._stream if stream is None else stream):  # (None: the current stream stays)
+            self._at.add_(1)
         self.length += 1
