@@ -214,6 +214,9 @@ class Continuations:
         """Append the next token of every continuation and attend; returns O."""
         if self.length >= self.max_new:
             raise ValueError(f"the tails hold {self.max_new} tokens")
+        N = self.fan[-1]
+        if isinstance(K, torch.Tensor) and K.shape[-3:-2] != (N,):  # (fewer would leave Q_dec laid out for fewer)
+            raise ValueError(f"K has shape {tuple(K.shape)}, a step takes a token of each of the {N} continuations")
         self._stream = stream
         E.ecokv_append(Q, K, V, self.ep.shape, self.rope, self.positions, None, self.rows, self.tails, self.Q_dec, stream)
         E.ecokv_decode_shared(self.Q_dec, self.ep.Kc, self.ep.Vc, self.ep.shape, self.fan, self.ep.counts, self.ep.offsets, self.max_count,

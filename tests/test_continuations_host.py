@@ -67,3 +67,17 @@ def test_advance_takes_a_stream(monkeypatch):
     co.step(*tokens(5), stream="s")
     co.advance(stream="t")
     assert rec.calls[-1] == ("advance", "t")
+
+
+def test_a_step_takes_one_token_of_every_continuation(monkeypatch):
+    # fewer would leave Q_dec, which the attention reads, laid out for fewer
+    rec = Recorder(monkeypatch)
+    co = continuations()
+    for n in (0, 1, 4, 6):
+        with pytest.raises(ValueError, match="5 continuations"):
+            co.step(*tokens(n))
+    with pytest.raises(ValueError, match="5 continuations"):
+        co.step(*(t[0, 0] for t in tokens(5)))
+    assert rec.calls == []
+    co.step(*(t[0] for t in tokens(5)))  # (one layer: without its dimension)
+    assert len(rec.calls) == 2
