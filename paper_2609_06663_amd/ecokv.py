@@ -120,23 +120,35 @@ class _Rope(ctypes.Structure):
                 ("k_norm", ctypes.c_void_p)]
 
 
+def _held(name: str):
+    """A handle's tensor.  The structure keeps its pointer from call to call, so
+    putting another in its place has the next call check that one and take its
+    pointer and sizes."""
+    def put(self, t):
+        self.__dict__[name] = t
+        self._for = None
+    return property(lambda self: self.__dict__[name], put)
+
+
 class Rope:
     """ecokv_rope: rotary positions (`freq` float32 [rot_dim / 2], see
     ecokv_rope_freqs) and, where `q_norm` / `k_norm` [D] weights are given, the
-    per-head norms before them.  Holds the tensors that it points to, whose
-    values may change but not their storage."""
+    per-head norms before them.  Holds the tensors that it points to: other
+    tensors may be assigned, and a tensor's values may change, but not its
+    storage."""
+
+    freq, q_norm, k_norm = _held("freq"), _held("q_norm"), _held("k_norm")
 
     def __init__(self, rot_dim: int, freq: Optional[torch.Tensor] = None, interleaved: bool = False, factor: float = 1.0,
                  q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, norm_eps: float = 1e-6):
         self.freq, self.q_norm, self.k_norm = freq, q_norm, k_norm
         self.c = _Rope(int(rot_dim), int(bool(interleaved)), None, factor, norm_eps, None, None)
 
-        self._for = None
-
     def _arg(self, head_dim: int, dtype, device):
         """Pointer to the structure, checked for rows of this size, element type and
-        device when these differ from the last call's."""
+        device when these differ from the last call's or a tensor was replaced."""
         if self._for != (head_dim, dtype, device):
+            self._for = None
             self.c.freq = _arg(self.freq, "freq", _F32, max(self.c.rot_dim, 0) // 2, device, optional=self.c.rot_dim <= 0)
             self.c.q_norm = _arg(self.q_norm, "q_norm", (dtype,), head_dim, device, optional=True)
             self.c.k_norm = _arg(self.k_norm, "k_norm", (dtype,), head_dim, device, optional=True)
@@ -152,25 +164,35 @@ class _Tails(ctypes.Structure):
 
 class Tails:
     """ecokv_tails: K, V [L][num_pages][H_kv][page_size][D] and table (int32)
-    [num_conts][max_pages].  Holds the tensors that it points to, whose values
-    may change but not their storage."""
+    [num_conts][max_pages].  Holds the tensors that it points to: others may be
+    assigned (a larger table or pool), and a tensor's values may change, but not
+    its storage."""
+
+    K, V, table = _held("K"), _held("V"), _held("table")
 
     def __init__(self, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor):
+        self.K, self.V, self.table = K, V, table
+        self.c = _Tails()
+        self._sizes()
+
+    def _sizes(self):
+        """The structure's sizes, those of the tensors."""
+        K, V, table = self.K, self.V, self.table
         if K.dim() != 5 or V.shape != K.shape or V.dtype != K.dtype:
             raise ValueError("the tails' K and V are two tensors [L][num_pages][H_kv][page_size][D] of one element type")
         if table.dim() != 2:
             raise ValueError("the tails' table is [num_conts][max_pages]")
-        self.K, self.V, self.table = K, V, table
-        self.c = _Tails(None, None, None, table.shape[0], K.shape[1], K.shape[3], table.shape[1])
-
-        self._for = None
+        c = self.c
+        c.num_conts, c.num_pages, c.page_size, c.max_pages = table.shape[0], K.shape[1], K.shape[3], table.shape[1]
 
     def _arg(self, shape: "Shape", dtype, device):
         """Pointer to the structure, checked for calls of this shape, element type
-        and device when these differ from the last call's."""
+        and device when these differ from the last call's or a tensor was replaced."""
         c = shape.c
         now = c.num_layers, c.num_kv_heads, c.head_dim, dtype, device
         if self._for != now:
+            self._for = None
+            self._sizes()
             L, _, H, _, D = self.K.shape
             if (L, H, D) != now[:3]:
                 raise ValueError(f"the tails have {L} layers of {H} KV heads of {D} dimensions, the shape "

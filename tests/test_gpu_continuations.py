@@ -57,3 +57,41 @@ def test_steps_on_a_stream_that_is_not_current(explicit):
             assert torch.equal(x, y), (i, name)
     assert torch.equal(co.tails.K, eager.tails.K) and torch.equal(co.tails.V, eager.tails.V)
     assert co.rows.tolist() == [4] * 5 and co.length == 4
+
+
+def test_tensors_of_the_handles_replaced_between_calls():
+    # a larger pool and table, other frequencies and norms: the next call reads those;
+    # the old ones are overwritten first, as memory that was given out again would be
+    import paper_2609_06663_amd as P
+    from test_gpu_rope import near, turned
+    from test_gpu_shared import Case
+    c = Case(61, "bf16", 1, 8, 2, 128, [[[300], [200]]], [3], [40, 1, 33], 16)
+    O, lse = c.run()
+    say("pool and table replaced")
+    pages, most = c.tk.shape[1], c.table.shape[1]
+    tk, tv = (torch.full_like(t, float("nan")) for t in (c.tk, c.tv))
+    t = P.Tails(tk, tv, torch.full_like(c.table, -1))
+    got, gl = torch.empty_like(O), torch.empty_like(lse)
+    call = lambda: P.ecokv_decode_shared(c.Q, c.Kc, c.Vc, c.shape, c.fan, c.counts, c.offsets, c.max_count, t, c.tail_counts, c.max_tail, got, gl)
+    call()
+    assert bool(got.isnan().all())
+    big = [torch.zeros(1, pages + 9, 2, 16, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    table = torch.full((3, most + 2), -1, dtype=torch.int32, device="cuda")
+    table[:, :most] = c.table + 9
+    for b, s in zip(big, (c.tk, c.tv)):
+        b[:, 9:] = s
+    t.table, (t.K, t.V) = table, big
+    call()
+    torch.cuda.synchronize()
+    assert torch.equal(got, O) and torch.equal(gl, lse)
+    say("frequencies and norms replaced")
+    g = torch.Generator(device="cuda").manual_seed(62)
+    K = torch.randn(1, 37, 2, 128, generator=g, device="cuda").bfloat16()
+    w = (1 + 0.1 * torch.randn(128, generator=g, device="cuda")).bfloat16()
+    f = [torch.rand(64, generator=g, device="cuda") for _ in range(2)]
+    shape, out = P.Shape(1, 4, 2, 128, 4, [0, 37]), torch.empty_like(K)
+    r = P.Rope(128, f[0])
+    for freq, norm in ((f[0], None), (f[1], None), (f[1], w), (f[0], None)):
+        r.freq, r.k_norm = freq, norm
+        P.ecokv_prefill_rope(None, K, shape, r, None, None, out)
+        near(out, *turned(K, torch.arange(37, device="cuda"), freq, 128, False, 1.0, norm, 1e-6), "bf16")
