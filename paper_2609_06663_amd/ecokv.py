@@ -120,6 +120,14 @@ class _Rope(ctypes.Structure):
                 ("k_norm", ctypes.c_void_p)]
 
 
+def _int32(v, name: str) -> int:
+    """v, which ctypes would cut to 32 bits without a word."""
+    v = int(v)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError(f"{name} {v} does not fit 32 bits")
+    return v
+
+
 def _held(name: str):
     """A handle's tensor.  The structure keeps its pointer from call to call, so
     putting another in its place has the next call check that one and take its
@@ -142,7 +150,7 @@ class Rope:
     def __init__(self, rot_dim: int, freq: Optional[torch.Tensor] = None, interleaved: bool = False, factor: float = 1.0,
                  q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, norm_eps: float = 1e-6):
         self.freq, self.q_norm, self.k_norm = freq, q_norm, k_norm
-        self.c = _Rope(int(rot_dim), int(bool(interleaved)), None, factor, norm_eps, None, None)
+        self.c = _Rope(_int32(rot_dim, "rot_dim"), int(bool(interleaved)), None, factor, norm_eps, None, None)
 
     def _arg(self, head_dim: int, dtype, device):
         """Pointer to the structure, checked for rows of this size, element type and
@@ -666,9 +674,10 @@ def _token_rows(t: Optional[torch.Tensor], name: str, dtype, want, device):
 def ecokv_rope_freqs(rot_dim: int, base: float = 10000.0, kind: int = ROPE_PLAIN, stretch: float = 1.0,
                      context: float = 0.0):
     """(frequencies as a list of rot_dim / 2 floats, factor) for Rope: radians per position of each pair."""
-    out = (ctypes.c_float * max(int(rot_dim) // 2, 1))()
+    rot_dim, kind = _int32(rot_dim, "rot_dim"), _int32(kind, "kind")
+    out = (ctypes.c_float * max(rot_dim // 2, 1))()
     factor = ctypes.c_float(0.0)
-    _check(lib.ecokv_rope_freqs(int(rot_dim), float(base), int(kind), float(stretch), float(context), out,
+    _check(lib.ecokv_rope_freqs(rot_dim, float(base), kind, float(stretch), float(context), out,
                                 ctypes.byref(factor)))
     return [float(v) for v in out], float(factor.value)
 
@@ -730,13 +739,16 @@ def _fan(shape: Shape, fan):
         fan = _flat_ints(fan)
         if len(fan) != n:
             raise ValueError("fan has one entry per prompt and one more")
-    return (ctypes.c_int32 * n)(*fan)
+    f = (ctypes.c_int32 * n)(*fan)
+    if f[:] != fan:
+        raise ValueError(f"fan {fan} does not fit 32 bits")
+    return f
 
 
 def ecokv_decode_shared_workspace_size(shape: Shape, fan: Sequence[int], max_count: int, max_tail: int) -> int:
     n = ctypes.c_size_t(0)
-    _check(lib.ecokv_decode_shared_workspace_size(ctypes.byref(shape.c), _fan(shape, fan), int(max_count),
-                                                  int(max_tail), ctypes.byref(n)))
+    _check(lib.ecokv_decode_shared_workspace_size(ctypes.byref(shape.c), _fan(shape, fan), _int32(max_count, "max_count"),
+                                                  _int32(max_tail, "max_tail"), ctypes.byref(n)))
     return n.value
 
 
@@ -757,6 +769,7 @@ def ecokv_decode_shared(Q_dec: torch.Tensor, Kc: Optional[torch.Tensor], Vc: Opt
     dev, dt, code = _first(Q_dec, "Q_dec")
     D = c.head_dim
     nq = c.num_layers * c.num_q_heads * N
+    max_count, max_tail = _int32(max_count, "max_count"), _int32(max_tail, "max_tail")
     kept, tailed = max_count > 0, max_tail > 0
     qp = _fit(Q_dec, "Q_dec", dt, nq * D, dev)
     kp, vp = _fit(Kc, "Kc", dt, D, dev, not kept), _fit(Vc, "Vc", dt, D, dev, not kept)
@@ -769,8 +782,8 @@ def ecokv_decode_shared(Q_dec: torch.Tensor, Kc: Optional[torch.Tensor], Vc: Opt
     units = shape.units
     _enqueue(lib.ecokv_decode_shared, dev, stream, qp, kp, vp, code, ctypes.byref(c), f,
              _fit(counts, "counts", torch.int32, units, dev, not kept), _fit(offsets, "offsets", torch.int32, units, dev, not kept),
-             int(max_count), tails._arg(shape, dt, dev) if tailed else None,
-             _fit(tail_counts, "tail_counts", torch.int32, N, dev, not tailed), int(max_tail),
+             max_count, tails._arg(shape, dt, dev) if tailed else None,
+             _fit(tail_counts, "tail_counts", torch.int32, N, dev, not tailed), max_tail,
              _fit(O, "O", torch.float32, nq * D, dev), _fit(lse, "lse", torch.float32, nq, dev, True),
              _fit(workspace, "workspace", torch.uint8, 0, dev), workspace.numel())
 

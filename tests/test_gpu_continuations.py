@@ -95,3 +95,14 @@ def test_tensors_of_the_handles_replaced_between_calls():
         r.freq, r.k_norm = freq, norm
         P.ecokv_prefill_rope(None, K, shape, r, None, None, out)
         near(out, *turned(K, torch.arange(37, device="cuda"), freq, 128, False, 1.0, norm, 1e-6), "bf16")
+
+
+def test_bounds_past_32_bits_are_refused():
+    import paper_2609_06663_amd as P
+    from test_gpu_shared import Case
+    c = Case(63, "f32", 1, 4, 2, 64, [[[30], [40]]], [2], [5, 6], 16)
+    O, lse = torch.empty(1, 4, 2, 64, device="cuda"), torch.empty(1, 4, 2, device="cuda")
+    t, ws = P.Tails(c.tk, c.tv, c.table), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    for mc, mt, fan in ((2 ** 32 + 40, 6, c.fan), (40, 2 ** 32, c.fan), (40, 6, [0, 2 ** 32 + 2])):
+        with pytest.raises(ValueError, match="32 bits"):
+            P.ecokv_decode_shared(c.Q, c.Kc, c.Vc, c.shape, fan, c.counts, c.offsets, mc, t, c.tail_counts, mt, O, lse, ws)

@@ -84,3 +84,22 @@ def test_rope_follows_its_tensors(E):
     r.freq = torch.ones(4, dtype=torch.float64)
     with pytest.raises(TypeError):
         r._arg(64, torch.bfloat16, None)
+
+
+def test_numbers_past_32_bits_are_refused():
+    # (ctypes cuts them to 32 bits: a bound of 2^32 would be one of 0, and the rows left out)
+    import paper_2609_06663_amd as P
+    s = P.Shape(1, 4, 2, 64, 4, [0, 10, 30])
+    size = lambda fan=(0, 1, 3), mc=5, mt=7: P.ecokv_decode_shared_workspace_size(s, list(fan), mc, mt)
+    assert size() > 0
+    for big in (2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 64 + 5, -2 ** 31 - 1, -2 ** 32 + 5):
+        for kw in (dict(fan=(0, 1, big)), dict(fan=(0, big, 3)), dict(fan=(big, 1, 3)), dict(mc=big), dict(mt=big)):
+            with pytest.raises(ValueError, match="32 bits"):
+                size(**kw)
+        with pytest.raises(ValueError, match="32 bits"):
+            P.Rope(big, torch.zeros(8))
+        with pytest.raises(ValueError, match="32 bits"):
+            P.ecokv_rope_freqs(16, 10000.0, big)
+    with pytest.raises(ValueError, match="32 bits"):
+        P.ecokv_rope_freqs(-2 ** 32 + 16)
+    size(mc=2 ** 31 - 1, mt=2 ** 31 - 1)
