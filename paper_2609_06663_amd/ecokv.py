@@ -772,18 +772,21 @@ def ecokv_decode_shared(Q_dec: torch.Tensor, Kc: Optional[torch.Tensor], Vc: Opt
     max_count, max_tail = _int32(max_count, "max_count"), _int32(max_tail, "max_tail")
     kept, tailed = max_count > 0, max_tail > 0
     qp = _fit(Q_dec, "Q_dec", dt, nq * D, dev)
-    kp, vp = _fit(Kc, "Kc", dt, D, dev, not kept), _fit(Vc, "Vc", dt, D, dev, not kept)
-    if kept and (Kc.numel() % D or Vc.numel() != Kc.numel()):
-        raise ValueError("Kc and Vc must hold the same whole number of rows of head_dim elements")
-    if tailed and tails is None:
-        raise ValueError("tails is required")
+    units = shape.units
+    # (what a bound of 0 leaves unread may be anything)
+    kp = vp = cp = op = tp = tc = None
+    if kept:
+        kp, vp = _fit(Kc, "Kc", dt, D, dev), _fit(Vc, "Vc", dt, D, dev)
+        if Kc.numel() % D or Vc.numel() != Kc.numel():
+            raise ValueError("Kc and Vc must hold the same whole number of rows of head_dim elements")
+        cp, op = _fit(counts, "counts", torch.int32, units, dev), _fit(offsets, "offsets", torch.int32, units, dev)
+    if tailed:
+        if tails is None:
+            raise ValueError("tails is required")
+        tp, tc = tails._arg(shape, dt, dev), _fit(tail_counts, "tail_counts", torch.int32, N, dev)
     if workspace is None:
         workspace = _workspace(None, ecokv_decode_shared_workspace_size(shape, fan, max_count, max_tail), dev, stream)
-    units = shape.units
-    _enqueue(lib.ecokv_decode_shared, dev, stream, qp, kp, vp, code, ctypes.byref(c), f,
-             _fit(counts, "counts", torch.int32, units, dev, not kept), _fit(offsets, "offsets", torch.int32, units, dev, not kept),
-             max_count, tails._arg(shape, dt, dev) if tailed else None,
-             _fit(tail_counts, "tail_counts", torch.int32, N, dev, not tailed), max_tail,
+    _enqueue(lib.ecokv_decode_shared, dev, stream, qp, kp, vp, code, ctypes.byref(c), f, cp, op, max_count, tp, tc, max_tail,
              _fit(O, "O", torch.float32, nq * D, dev), _fit(lse, "lse", torch.float32, nq, dev, True),
              _fit(workspace, "workspace", torch.uint8, 0, dev), workspace.numel())
 

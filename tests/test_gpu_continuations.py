@@ -106,3 +106,24 @@ def test_bounds_past_32_bits_are_refused():
     for mc, mt, fan in ((2 ** 32 + 40, 6, c.fan), (40, 2 ** 32, c.fan), (40, 6, [0, 2 ** 32 + 2])):
         with pytest.raises(ValueError, match="32 bits"):
             P.ecokv_decode_shared(c.Q, c.Kc, c.Vc, c.shape, fan, c.counts, c.offsets, mc, t, c.tail_counts, mt, O, lse, ws)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f32", 64)])
+def test_what_a_bound_of_zero_leaves_unread_may_be_empty(dtype, D):
+    # the cache of prompts of which nothing was kept, the counts of tails not yet begun
+    import paper_2609_06663_amd as P
+    from test_gpu_shared import Case
+    c = Case(64, dtype, 1, 4, 2, D, [[[30], [0]]], [2], [5, 6], 16)
+    O, lse = torch.empty(1, 4, 2, D, device="cuda"), torch.empty(1, 4, 2, device="cuda")
+    none, no_counts = c.Kc[:0], c.counts[:0]
+    say(f"{dtype} D={D}: nothing kept")
+    P.ecokv_decode_shared(c.Q, none, none, c.shape, c.fan, no_counts, no_counts, 0, P.Tails(c.tk, c.tv, c.table), c.tail_counts, 6, O, lse)
+    want = c.run(max_count=0)
+    assert torch.equal(O, want[0]) and torch.equal(lse, want[1])
+    say(f"{dtype} D={D}: no tails")
+    P.ecokv_decode_shared(c.Q, c.Kc, c.Vc, c.shape, c.fan, c.counts, c.offsets, 30, None, no_counts, 0, O, lse)
+    want = c.run(max_tail=0)
+    assert torch.equal(O, want[0]) and torch.equal(lse, want[1])
+    say(f"{dtype} D={D}: neither")
+    P.ecokv_decode_shared(c.Q, none, none, c.shape, c.fan, no_counts, no_counts, 0, None, no_counts, 0, O, lse)
+    assert bool((O == 0).all()) and bool((lse == -float("inf")).all())
