@@ -1,4 +1,5 @@
-"""Sizes at which ecokv_decode_shared takes its wide query tiles over long parts: run on the GPU by
+"""Sizes at which ecokv_decode_shared takes its wide query tiles over long parts,
+and sizes past one dimension of its grids: run on the GPU by
 tests/test_gpu_shared_wide.py, their splits checked on the host by
 tests/test_shared_plan_wide.py."""
 
@@ -26,6 +27,12 @@ def kept(case):
     _, _, L, _, Hkv, counts, _, _, _ = case
     return [[[n if (l, h) == (0, 0) else 1 if (l, h) == (1, 0) else n - 37 * ((5 * h + 3 * l + s) % 41) * n // 4000
               for s, n in enumerate(counts)] for h in range(Hkv)] for l in range(L)]
+
+
+# L, Hq, Hkv, D, number of prompts (each continued once) or continuations of one, max_count, max_tail
+GRID_TAILS = (2, 64, 64, 128, 65_600, 0, 1)             # tails, and the merge of a row's few partials
+GRID_PROMPTS = (260, 64, 64, 64, 64, 1, 0)              # prompts' blocks
+GRID_MERGE = (260, 64, 64, 64, 64, 25 << 22, 0)         # the merge of many partials, 25 million blocks
 
 # rows that a head of 4 keeps on average where they share a budget, the most that one may, and a wave's of them
 SHARED_BUDGET = 1600

@@ -1,6 +1,6 @@
 """ecokv_decode_shared where a call is large: query tiles of two and four waves
 over parts of many tiles (tests/test_gpu_shared.py reaches these tiles with one or
-two).  The splits that the sizes are there for are
+two), and grids past one dimension.  The splits that the sizes are there for are
 checked on the host, tests/test_shared_plan_wide.py.
 
 Tolerance: that of tests/test_gpu_shared.py, whose 64 roundings of sums hold for
@@ -14,7 +14,7 @@ import sys
 
 import pytest
 import torch
-from shared_sizes import SHARED_BOUND, SHARED_BUDGET, SHARED_WAVE, TAIL, WIDE, kept
+from shared_sizes import GRID_MERGE, GRID_PROMPTS, GRID_TAILS, SHARED_BOUND, SHARED_BUDGET, SHARED_WAVE, TAIL, WIDE, kept
 
 pytestmark = pytest.mark.gpu
 
@@ -72,6 +72,54 @@ def test_wide_tiles_over_long_parts(case):
     # and the same bits again
     O2, lse2 = c.run()
     assert torch.equal(O, O2) and torch.equal(lse, lse2)
+
+
+def one_row_each(Q, K, V, O, lse):
+    """Outputs of query rows Q [..., D] that attend one row each, K and V: the value itself, and the logit."""
+    D = Q.shape[-1]
+    assert bool(((O - V.float()).abs() <= 2.0 ** -20 * V.float().abs()).all())
+    q, k = Q.double(), K.double()
+    bound = 40 * 2.0 ** -24 * (q.abs() * k.abs()).sum(-1) / D ** 0.5
+    x = (q * k).sum(-1) / D ** 0.5
+    assert bool(((lse.double() - x).abs() <= bound + 2.0 ** -20 * x.abs().clamp_min(1)).all())
+
+
+def test_more_tails_than_one_dimension_holds():
+    # every query row has a value of its own, so that one in another's place shows
+    import paper_2609_06663_amd as P
+    L, Hq, Hkv, D, N, _, mt = GRID_TAILS
+    say(f"{L * Hkv * N} tails of one row")
+    g = torch.Generator(device="cuda").manual_seed(71)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda", dtype=torch.bfloat16)
+    Q, tk, tv = r(L, Hq, N, D), r(L, N, Hkv, 1, D), r(L, N, Hkv, 1, D)
+    table = torch.randperm(N, generator=torch.Generator().manual_seed(72)).int().cuda().view(N, 1)
+    ones = torch.ones(N, dtype=torch.int32, device="cuda")
+    O, lse = torch.full((L, Hq, N, D), -7.0, device="cuda"), torch.full((L, Hq, N), -7.0, device="cuda")
+    P.ecokv_decode_shared(Q, None, None, P.Shape(L, Hq, Hkv, D, 4, [0, 10]), [0, N], None, None, 0, P.Tails(tk, tv, table), ones, mt, O, lse)
+    torch.cuda.synchronize()
+    at = table.view(-1).long()
+    for l in range(L):
+        for h in range(Hkv):
+            one_row_each(Q[l, h], tk[l, at, h, 0], tv[l, at, h, 0], O[l, h], lse[l, h])
+
+
+@pytest.mark.parametrize("size", [GRID_PROMPTS, GRID_MERGE], ids=str)
+def test_more_prompts_than_one_dimension_holds(size):
+    import paper_2609_06663_amd as P
+    L, Hq, Hkv, D, B, mc, _ = size
+    units = L * Hkv * B
+    say(f"{units} units of one row, bound {mc}")
+    g = torch.Generator(device="cuda").manual_seed(73)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda", dtype=torch.bfloat16)
+    Q, Kc, Vc = r(L, Hq, B, D), r(units, D), r(units, D)
+    offsets = torch.randperm(units, generator=torch.Generator().manual_seed(74)).int().cuda()
+    ones = torch.ones(units, dtype=torch.int32, device="cuda")
+    O, lse = torch.full((L, Hq, B, D), -7.0, device="cuda"), torch.full((L, Hq, B), -7.0, device="cuda")
+    P.ecokv_decode_shared(Q, Kc, Vc, P.Shape(L, Hq, Hkv, D, 4, [10 * s for s in range(B + 1)]), list(range(B + 1)), ones, offsets, mc, None, None, 0, O, lse)
+    torch.cuda.synchronize()
+    at = offsets.view(L, Hkv, B).long()
+    for l in range(L):
+        one_row_each(Q[l], Kc[at[l]], Vc[at[l]], O[l], lse[l])
 
 
 def test_generation_from_prompts_whose_heads_share_a_budget():
