@@ -411,6 +411,8 @@ typedef struct ecokv_rope {
                               /* `context` positions as they are, those that turn */
                               /* at most once divided by stretch, a linear ramp   */
                               /* over the turns between; factor 0.1 ln stretch + 1 */
+/* A model whose ramp has other limits, or is linear in the pair's index, or whose
+ * factor is another, brings its own table in ecokv_rope.freq. */
 
 /* Host only: the frequencies of rot_dim / 2 pairs into freq (HOST) and the
  * factor of cosines and sines into *factor (1 but for BY_PARTS).  ECOKV_EINVAL

@@ -702,6 +702,15 @@ __device__ __forceinline__ void write_out(const SharedArgs &a, uint32_t qrow, in
 // workspace loaded at once, ahead of the counts that say which hold a partial
 // (the others' contents are not used).  A call without kept rows and tails has
 // no places.
+// The forms load FEW places whatever a call has, so a call takes the next one up,
+// and past the last k_shared_merge.  us a merge out of a graph, D = 128, forms of
+// 2, 3, 5, 8, 14, 24 places and a block a row: 1792 query rows, 2 partials 2.6 2.7
+// 2.9 3.1 3.6 4.5 5.7, 5 partials - - 3.2 3.4 4.0 4.8 6.1, 12 - - - - 4.8 5.7 6.2,
+// 20 - - - - - 6.6 6.2, 24 7.0 and 6.2; 12544 rows, 2 partials 4.6 4.9 5.5 6.5 9.0
+// 15.9 22.8, 5 - - 7.2 8.0 10.6 18.3 25.7, 12 - - - - 16.1 25.3 26.6, 24 34 and 28
+// (D = 64: 21 and 28).  The rule does not look at the rows: with few of them a block
+// a row is as fast from 6 to 8 partials on (224 rows: 6 partials 3.4 3.5, 12 4.7 3.5, 20
+// 6.4 3.5).
 constexpr int kShMergeThreads = 256, kShFew = 24;
 template <int D, int FEW>
 __global__ __launch_bounds__(kShMergeThreads) void k_shared_merge_few(SharedArgs a)

@@ -161,7 +161,9 @@ class Continuations:
     views of a fused tensor will do), norms and rotates queries and keys (`rope`),
     appends keys and values and attends: O [L][H_q][N][D] float32 and lse; then
     `advance` moves on.  Positions go on from the prompts' own lengths, whatever
-    was evicted.  The pass may hold one layer or several; with a pass per layer,
+    was evicted.  All continuations go on together: one that has ended keeps its
+    place, with any token and its output unused (`rows`, `tail_counts` and
+    `positions` are advanced for all).  The pass may hold one layer or several; with a pass per layer,
     each layer has its own instance, advanced with the others.
 
     `step` and `advance` only enqueue work, on one stream at a time (they share a
