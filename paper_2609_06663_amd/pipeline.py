@@ -163,15 +163,17 @@ class Continuations:
     `advance` moves on.  Positions go on from the prompts' own lengths, whatever
     was evicted.  All continuations go on together: one that has ended keeps its
     place, with any token and its output unused (`rows`, `tail_counts` and
-    `positions` are advanced for all).  The pass may hold one layer or several; with a pass per layer,
-    each layer has its own instance, advanced with the others.
+    `positions` are advanced for all).  The pass may hold one layer or several;
+    with a pass per layer, each layer has its own instance, advanced with the
+    others.
 
     `step` and `advance` only enqueue work, on one stream at a time (they share a
     workspace): `advance` goes where the last `step` went, to the stream that it
     was given or else to the current one.  Who changes the stream between calls
-    orders the one after the other.  To capture them in a HIP graph, pass `step` max_tail=max_new: by
-    default it is the present length, which a replay would not raise.  A replay
-    moves the device's counters only; `length` is the caller's to keep."""
+    orders the one after the other.  To capture them in a HIP graph, pass `step`
+    max_tail=max_new: by default it is the present length, which a replay would
+    not raise.  A replay moves the device's counters only; `length` is the
+    caller's to keep."""
 
     def __init__(self, ep: EvictionPass, fan_out, max_new: int, rope: E.Rope, page_size: int = 64):
         shape = ep.shape
