@@ -16,7 +16,10 @@
  *                 (Sec. 3, selected subset).
  * Before it: ecokv_prefill_rope (norms and rotary positions) and
  * ecokv_prefill_write (the cache write); after it: ecokv_decode, or
- * ecokv_append and ecokv_decode_shared for continuations of the prompts.
+ * ecokv_append and ecokv_decode_shared for continuations of the prompts
+ * (ecokv_decode_tree and ecokv_commit where several drafted tokens are
+ * verified at a time), and ecokv_accumulate, ecokv_evict and
+ * ecokv_evict_tails to keep the cache bounded meanwhile.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -94,6 +97,7 @@ extern "C" {
 
 #define ECOKV_MAX_SEQS 64   /* sequences per call                              */
 #define ECOKV_MAX_ROWS 64   /* window rows per KV head, (H_q/H_kv)*w           */
+#define ECOKV_MAX_NODES 64  /* drafted tokens of a continuation per call       */
 
 /* Per-unit statistics written by ecokv_score when `stats` is non-NULL. */
 #define ECOKV_STAT_LAMBDA 0    /* lambda = beta r_E + (1-beta) r_C, Eq. (6)      */
@@ -517,6 +521,145 @@ int ecokv_decode_shared(const void *Q_dec, const void *Kc, const void *Vc, int d
                         const int32_t *fan, const int32_t *counts, const int32_t *offsets, int32_t max_count,
                         const ecokv_tails *tails, const int32_t *tail_counts, int32_t max_tail, float *O, float *lse,
                         void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- Several drafted tokens at a time ----
+ *
+ * A draft proposes a tree of tokens behind each continuation: node i's parent is
+ * an earlier node, or the last token of the tail.  One pass of the model over all
+ * nodes verifies them.  In every layer: ecokv_append writes the nodes' keys and
+ * values behind the tail (row tail_counts[c] + i, at the position after the tail's
+ * last plus the node's depth), ecokv_decode_tree attends; then one ecokv_commit
+ * over all layers puts the rows of the accepted path in order, and the caller adds
+ * accepted[c] to the tail's rows and positions. */
+
+/* Host only: what each node of a tree sees.  parents (HOST [num_nodes]): -1, or an
+ * earlier node.  masks (HOST [num_nodes]): bit j of masks[i] is set if node j is node
+ * i or one of its ancestors; depths (HOST [num_nodes], or NULL): ancestors of each
+ * node.  ECOKV_EINVAL for other parents, or num_nodes outside [1, ECOKV_MAX_NODES]. */
+int ecokv_tree_masks(int num_nodes, const int32_t *parents, uint64_t *masks, int32_t *depths);
+
+/* Workspace bytes of ecokv_decode_tree for this shape, fan and these bounds, as
+ * ecokv_decode_shared_workspace_size (smaller bounds may need more). */
+int ecokv_decode_tree_workspace_size(const ecokv_shape *shape, const int32_t *fan, int32_t max_count, int32_t max_tail,
+                                     int32_t num_nodes, size_t *bytes);
+
+/* Attention of num_nodes drafted tokens of each of N continuations: over its
+ * prompt's kept rows, its tail and those of its drafted rows that their mask names.
+ *   shape, fan, Kc, Vc, counts, offsets, max_count
+ *           as for ecokv_decode_shared
+ *   tails, tail_counts
+ *           tail_counts (DEVICE [N]): rows of each tail, all seen by every node;
+ *           drafted row i of continuation c is row tail_counts[c] + i of its tail
+ *   max_tail  an upper bound of every tail_counts[c], at most max_pages * page_size
+ *   masks   DEVICE [N][num_nodes]: node i of continuation c sees its drafted row j
+ *           if bit j of masks[c][i] is set (any bits will do, also j > i, and a node
+ *           need not see itself; bits from num_nodes on are ignored)
+ *   Q_dec   DEVICE [L][H_q][N num_nodes][D] (dtype), node i of continuation c at
+ *           c num_nodes + i, as ecokv_append writes them for tokens in this order
+ *   O       DEVICE [L][H_q][N num_nodes][D] of type dtype, rounded once at the end;
+ *           lse DEVICE [L][H_q][N num_nodes] float32, or NULL; 0 and -inf for a node
+ *           that sees no row
+ * A drafted row that a node does not see does not reach its outputs, whatever the row
+ * holds, and need not exist: trees of fewer nodes leave the last masks 0 and those
+ * rows unwritten.  A tail row without a page in [0, num_pages) gives NaN outputs for
+ * its continuation, a drafted row without one for the nodes that see it, a count out
+ * of its bounds for the continuations concerned.
+ * Arithmetic: fp32 accumulation (bf16 rows: the weights as two bf16 summands each, 16
+ * bits, beside an output of 8; among kept rows and the tail's a value row with an
+ * infinity gives NaN).
+ * Alignment, workspace and repeatability as ecokv_decode_shared; outputs and the
+ * workspace overlap neither Q_dec nor the tails nor each other. */
+int ecokv_decode_tree(const void *Q_dec, const void *Kc, const void *Vc, int dtype, const ecokv_shape *shape,
+                      const int32_t *fan, const int32_t *counts, const int32_t *offsets, int32_t max_count,
+                      const ecokv_tails *tails, const int32_t *tail_counts, int32_t max_tail, int32_t num_nodes,
+                      const uint64_t *masks, void *O, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The rows of the accepted path of each tree to the end of its tail: for k <
+ * accepted[c], row tail_counts[c] + path[c][k] goes to row tail_counts[c] + k, for
+ * every layer and KV head.
+ *   shape   only num_layers, num_kv_heads and head_dim are read
+ *   tail_counts  DEVICE [N], before the accepted rows are added; not written
+ *   path    DEVICE [N][num_nodes], the accepted nodes in ascending order
+ *   accepted  DEVICE [N], 0 .. num_nodes
+ * A continuation whose count is negative, whose accepted[c] is not in
+ * [0, num_nodes], whose path does not ascend within [0, num_nodes) or one of whose
+ * rows has no page is left as it is.  Pages that are written belong to one
+ * continuation alone. */
+int ecokv_commit(int dtype, const ecokv_shape *shape, const ecokv_tails *tails, const int32_t *tail_counts,
+                 int32_t num_nodes, const int32_t *path, const int32_t *accepted, void *stream);
+
+/* ---- A cache that stays bounded while it generates ----
+ *
+ * ecokv_accumulate adds up, over the steps, the attention weight of every row;
+ * ecokv_evict (prompts) and ecokv_evict_tails (continuations) drop the rows of the
+ * least weight once there are more than a limit.  The masses are float32: one per row
+ * of the compressed cache, and [L][num_pages][H_kv][page_size] for the tails. */
+
+/* After the attention of a step: every row's mass is multiplied by decay, and the
+ * weights that the row got are added, summed over the query heads of its KV head's
+ * group and over the queries that see it:
+ *   out = decay in + sum of exp(q . k / sqrt(D) - lse).
+ *   Q_dec   DEVICE [L][H_q][N num_nodes][D] (dtype), as the attention read it
+ *   lse     DEVICE [L][H_q][N num_nodes], as the attention left it
+ *   shape, fan, Kc, counts, offsets, max_count, tails, max_tail
+ *           as for ecokv_decode_shared; either bound may be 0 (that set of rows is then
+ *           left alone, and its arguments may be NULL)
+ *   tail_counts  DEVICE [N]: rows of each tail, the new ones included
+ *   path, accepted  NULL after ecokv_decode_shared (num_nodes = 1: one query of each
+ *           continuation, which sees all its rows, the last of them new).  After
+ *           ecokv_decode_tree and ecokv_commit, what the latter was given, with
+ *           tail_counts as the caller advanced them: the queries are the nodes
+ *           path[c][k], k < accepted[c], and the k-th sees the tail's rows up to its own,
+ *           tail_counts[c] - accepted[c] + k.
+ *   decay   finite, >= 0
+ *   mass, mass_out  DEVICE, one value for each row of Kc (mass_out may be mass)
+ *   tail_mass, tail_mass_out  DEVICE [L][num_pages][H_kv][page_size] (likewise).  The
+ *           new rows begin with what they get now: their old masses are not read.
+ * Only rows of the units and tails are read and written.  A prompt's or tail's rows are
+ * left alone where its count is out of its bounds, and a tail row without a page is
+ * skipped; a path's entry outside [0, num_nodes) adds nothing, nor does a query whose
+ * lse is -inf.  A page whose masses are kept belongs to one continuation alone.
+ * Arithmetic: fp32 (weights below 2^-126 count as 0).  The same call gives the same bits. */
+int ecokv_accumulate(const void *Q_dec, const float *lse, const void *Kc, int dtype, const ecokv_shape *shape,
+                     const int32_t *fan, const int32_t *counts, const int32_t *offsets, int32_t max_count,
+                     const ecokv_tails *tails, const int32_t *tail_counts, int32_t max_tail, int32_t num_nodes,
+                     const int32_t *path, const int32_t *accepted, float decay, const float *mass, const float *tail_mass,
+                     float *mass_out, float *tail_mass_out, void *stream);
+
+/* Workspace bytes of ecokv_evict (groups: the shape's sequences) and
+ * ecokv_evict_tails (groups: the continuations) for a bound of max_rows rows of which
+ * `keep` stay.  Larger keeps may need less. */
+int ecokv_evict_workspace_size(const ecokv_shape *shape, int32_t groups, int32_t max_rows, int32_t keep, size_t *bytes);
+
+/* Eviction from the compressed cache.  A unit u with n = counts[u] > limit rows keeps
+ * `keep` of them: the last `recent`, and of the others the keep - recent of the largest
+ * mass (equal masses: the lower row; NaN below every number, -0 equal to +0).  In place:
+ *   rows 0 .. keep - recent - 1 that stay are not moved; the places of those that go are
+ *   filled, in ascending order, by the rows from keep - recent on that stay, ascending;
+ *   the last `recent` rows follow in their order, to row keep - 1.
+ * Their masses go with them, to mass_out.  Units with fewer rows stay as they are (where
+ * mass_out is not mass, their masses are copied); so does, masses and all, a unit whose
+ * count is negative or above max_count.
+ *   Kc, Vc, counts, offsets, max_count  as for ecokv_decode; no two units share rows
+ *   limit, keep, recent   1 <= keep <= limit, 0 <= recent <= keep
+ *   mass, mass_out  DEVICE, one value for each row of Kc; mass_out may be mass, or else
+ *           does not overlap it; from row `keep` of a unit on it is not written
+ *   new_counts  DEVICE [L][H_kv][B], the rows afterwards; may be counts
+ *   workspace  DEVICE, >= ecokv_evict_workspace_size bytes, 256-byte aligned; no initial
+ *           contents needed, one call at a time
+ * offsets stay valid.  Errors as the other entry points; nothing is enqueued then. */
+int ecokv_evict(void *Kc, void *Vc, int dtype, const ecokv_shape *shape, const int32_t *counts, const int32_t *offsets,
+                int32_t max_count, int32_t limit, int32_t keep, int32_t recent, const float *mass, float *mass_out,
+                int32_t *new_counts, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The same for the tails: a continuation with more than `limit` rows keeps `keep`, every
+ * (layer, KV head) its own.  new_counts: DEVICE [N], may be tail_counts.  Of the shape
+ * num_layers, num_kv_heads and head_dim are read.  Positions go on as if nothing had gone.  A
+ * continuation any of whose rows has no page in [0, num_pages) stays as it is; pages that are
+ * written belong to one continuation alone. */
+int ecokv_evict_tails(int dtype, const ecokv_shape *shape, const ecokv_tails *tails, const int32_t *tail_counts,
+                      int32_t max_tail, int32_t limit, int32_t keep, int32_t recent, const float *tail_mass,
+                      float *tail_mass_out, int32_t *new_counts, void *workspace, size_t workspace_bytes, void *stream);
 
 /* PyramidKV's layer schedule (Appendix A.1), host only: for m = num_layers
  * layers sharing `total` tokens per head, the last layer gets

@@ -17,7 +17,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libecokv.so")
 SOURCES = ["ecokv_api.hip", "ecokv_score.hip", "ecokv_sweep.hip", "ecokv_select.hip", "ecokv_compact.hip", "ecokv_decode.hip",
-           "ecokv_rope.hip", "ecokv_shared.hip"]
+           "ecokv_rope.hip", "ecokv_shared.hip", "ecokv_tree.hip", "ecokv_accumulate.hip", "ecokv_evict.hip"]
 ARCH = "gfx950"
 
 # Packed-fp32 instructions are disabled for every HIP translation unit.

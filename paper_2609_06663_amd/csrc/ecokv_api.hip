@@ -940,6 +940,77 @@ int check_fan(const ShapeInfo &si, const int32_t *fan)
     return ECOKV_OK;
 }
 
+// Arguments of a call with num_nodes queries of each continuation; nodes: fan times
+// num_nodes.
+int check_tree(const ShapeInfo &si, const int32_t *fan, int32_t max_count, int32_t max_tail, int32_t num_nodes, int32_t *nodes)
+{
+    const int rc = check_fan(si, fan);
+    if (rc) return rc;
+    if (num_nodes < 1 || num_nodes > ECOKV_MAX_NODES)
+        return fail(ECOKV_EINVAL, "num_nodes %d outside [1, %d]", num_nodes, ECOKV_MAX_NODES);
+    if (max_count < 0 || max_tail < 0) return fail(ECOKV_EINVAL, "max_count %d or max_tail %d < 0", max_count, max_tail);
+    if (max_tail > INT32_MAX - ECOKV_MAX_NODES) return fail(ECOKV_EINVAL, "max_tail %d", max_tail);
+    if ((int64_t)(si.L > 0 ? si.L : 1) * si.Hq * num_nodes > (int64_t)INT32_MAX / (fan[si.B] > 0 ? fan[si.B] : 1))
+        return fail(ECOKV_EINVAL, "too many (layer, query head, node) rows");
+    for (int s = 0; s <= si.B; ++s) nodes[s] = fan[s] * num_nodes;
+    return ECOKV_OK;
+}
+
+int check_tail_counts(const ecokv_tails *tails, int conts, const int32_t *tail_counts, int32_t max_tail)
+{
+    if (!tail_counts) return fail(ECOKV_EINVAL, "tail_counts must be non-NULL");
+    if (tails->num_conts != conts) return fail(ECOKV_EINVAL, "the tails have %d continuations, the call %d", tails->num_conts, conts);
+    if ((int64_t)max_tail > (int64_t)tails->max_pages * tails->page_size)
+        return fail(ECOKV_EINVAL, "max_tail %d is more rows than %d pages of %d hold", max_tail, tails->max_pages,
+                    tails->page_size);
+    return ECOKV_OK;
+}
+
+// The masses of the tails' rows: one buffer, or two that do not overlap.
+int check_tail_mass(const ecokv_tails *t, const ShapeInfo &si, const float *in, float *out)
+{
+    if (!in || !out) return fail(ECOKV_EINVAL, "tail_mass and tail_mass_out must be non-NULL");
+    const size_t n = sizeof(float) * (size_t)si.L * t->num_pages * si.Hkv * (size_t)t->page_size;
+    if (in != out && overlap(Span{in, n}, Span{out, n}))
+        return fail(ECOKV_EINVAL, "tail_mass_out overlaps tail_mass and is not the same");
+    return ECOKV_OK;
+}
+
+int check_evict(const ShapeInfo &si, int groups, int32_t max_rows, int32_t limit, int32_t keep, int32_t recent)
+{
+    if (max_rows < 0) return fail(ECOKV_EINVAL, "a bound of %d rows", max_rows);
+    if (keep < 1 || limit < keep) return fail(ECOKV_EINVAL, "keep %d is below 1 or above the limit %d", keep, limit);
+    if (recent < 0 || recent > keep) return fail(ECOKV_EINVAL, "recent %d outside [0, keep = %d]", recent, keep);
+    if ((int64_t)si.L * si.Hkv * groups > INT32_MAX / 64) return fail(ECOKV_EINVAL, "too many (layer, KV head, group) units");
+    return ECOKV_OK;
+}
+
+int evict_impl(ecokv::EvictArgs a, const ShapeInfo &si, int groups, int dtype, int32_t limit, int32_t keep, int32_t recent,
+               const float *mass, float *mass_out, int32_t *new_counts, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int64_t words = ecokv::evict_plan_words(a.max_rows, keep);
+    a.units = (int64_t)si.L * si.Hkv * groups;
+    const size_t need = sizeof(int) * (size_t)a.units * (size_t)words;
+    if (!workspace) return fail(ECOKV_EINVAL, "workspace is NULL");
+    if (((uintptr_t)workspace & 255u) != 0) return fail(ECOKV_EINVAL, "workspace must be 256-byte aligned");
+    if (workspace_bytes < need) return fail(ECOKV_EWORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
+    a.mass = mass;
+    a.mass_out = mass_out;
+    a.new_counts = new_counts;
+    a.plan = static_cast<int *>(workspace);
+    a.Hkv = si.Hkv;
+    a.groups = groups;
+    a.row_bytes = si.D * (dtype == ECOKV_BF16 ? 2 : 4);
+    a.limit = limit;
+    a.keep = keep;
+    a.recent = recent;
+    a.cap = ecokv::evict_plan_cap(a.max_rows, keep);
+    a.plan_stride = words;
+    const hipError_t e = ecokv::evict_launch(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "eviction launch");
+    return ECOKV_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1141,6 +1212,278 @@ int ecokv_decode_shared(const void *Q_dec, const void *Kc, const void *Vc, int d
     const hipError_t e = ecokv::shared_launch(a, dtype == ECOKV_BF16, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "ecokv_decode_shared launch");
     return ECOKV_OK;
+}
+
+int ecokv_tree_masks(int num_nodes, const int32_t *parents, uint64_t *masks, int32_t *depths)
+{
+    if (num_nodes < 1 || num_nodes > ECOKV_MAX_NODES)
+        return fail(ECOKV_EINVAL, "num_nodes %d outside [1, %d]", num_nodes, ECOKV_MAX_NODES);
+    if (!parents || !masks) return fail(ECOKV_EINVAL, "parents and masks must be non-NULL");
+    for (int i = 0; i < num_nodes; ++i)
+        if (parents[i] < -1 || parents[i] >= i)
+            return fail(ECOKV_EINVAL, "parents[%d] = %d is neither -1 nor an earlier node", i, parents[i]);
+    for (int i = 0; i < num_nodes; ++i) {
+        const int p = parents[i];
+        masks[i] = (p >= 0 ? masks[p] : 0) | (uint64_t)1 << i;
+        if (depths) depths[i] = p >= 0 ? depths[p] + 1 : 0;
+    }
+    return ECOKV_OK;
+}
+
+int ecokv_decode_tree_workspace_size(const ecokv_shape *shape, const int32_t *fan, int32_t max_count, int32_t max_tail,
+                                     int32_t num_nodes, size_t *bytes)
+{
+    ShapeInfo si;
+    int32_t nodes[ECOKV_MAX_SEQS + 1];
+    int rc = check_shape(shape, &si);
+    if (rc) return rc;
+    if ((rc = check_tree(si, fan, max_count, max_tail, num_nodes, nodes))) return rc;
+    if (!bytes) return fail(ECOKV_EINVAL, "bytes is NULL");
+    ecokv::TreeTails tails;
+    *bytes = 0;
+    for (int bf16 = 0; bf16 < 2; ++bf16) {  // the element type changes the split; report the larger
+        const size_t n = ecokv::tree_grid((int64_t)si.L * si.Hkv, si.G, si.D, si.B, nodes, fan[si.B], num_nodes, max_count,
+                                          max_tail, bf16 != 0, &tails).bytes;
+        if (n > *bytes) *bytes = n;
+    }
+    return ECOKV_OK;
+}
+
+int ecokv_decode_tree(const void *Q_dec, const void *Kc, const void *Vc, int dtype, const ecokv_shape *shape,
+                      const int32_t *fan, const int32_t *counts, const int32_t *offsets, int32_t max_count,
+                      const ecokv_tails *tails, const int32_t *tail_counts, int32_t max_tail, int32_t num_nodes,
+                      const uint64_t *masks, void *O, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    ShapeInfo si;
+    ecokv::TreeArgs a;
+    memset(&a, 0, sizeof a);
+    ecokv::SharedArgs &s = a.s;
+    int rc = check_shape(shape, &si);
+    if (rc) return rc;
+    if (dtype != ECOKV_BF16 && dtype != ECOKV_F32) return fail(ECOKV_EUNSUPPORTED, "dtype %d", dtype);
+    if ((rc = check_tree(si, fan, max_count, max_tail, num_nodes, s.fan))) return rc;
+    if (si.L == 0 || fan[si.B] == 0) return ECOKV_OK;
+    const bool bf16 = dtype == ECOKV_BF16;
+    const size_t rows = (size_t)si.L * si.Hq * s.fan[si.B], q = rows * si.D * (bf16 ? 2 : 4);
+    if (!Q_dec || !O || !masks) return fail(ECOKV_EINVAL, "Q_dec, masks and O must be non-NULL");
+    if (max_count > 0 && (!Kc || !Vc || !counts || !offsets))
+        return fail(ECOKV_EINVAL, "Kc, Vc, counts and offsets must be non-NULL");
+    if ((((uintptr_t)Q_dec | (uintptr_t)Kc | (uintptr_t)Vc | (uintptr_t)O) & 15u) != 0)
+        return fail(ECOKV_EINVAL, "Q_dec, Kc, Vc and O must be 16-byte aligned");
+    Span tk, tv;
+    if ((rc = check_tails(tails, si, bf16 ? 2 : 4, &s.map, &tk, &tv))) return rc;
+    if ((rc = check_tail_counts(tails, fan[si.B], tail_counts, max_tail))) return rc;
+    const Span so{O, q}, sl{lse, rows * 4}, sw{workspace, workspace_bytes}, in[3] = {Span{Q_dec, q}, tk, tv};
+    for (int i = 0; i < 3; ++i)
+        if (overlap(in[i], so) || overlap(in[i], sl) || overlap(in[i], sw))
+            return fail(ECOKV_EINVAL, "O, lse or the workspace overlaps Q_dec or the tails");
+    if (overlap(so, sl) || overlap(so, sw) || overlap(sl, sw)) return fail(ECOKV_EINVAL, "O, lse and the workspace overlap");
+    s.grid = ecokv::tree_grid((int64_t)si.L * si.Hkv, si.G, si.D, si.B, s.fan, fan[si.B], num_nodes, max_count, max_tail, bf16,
+                              &a.tails);
+    if (s.grid.prompt_blocks > INT32_MAX - (1 << 20) || s.grid.tail_waves > INT32_MAX - (1 << 20) ||
+        a.tails.blocks > INT32_MAX - (1 << 20) - s.grid.prompt_blocks)
+        return fail(ECOKV_EINVAL, "too many parts of kept rows or tails");
+    if (!workspace) return fail(ECOKV_EINVAL, "workspace is NULL");
+    if (((uintptr_t)workspace & 255u) != 0) return fail(ECOKV_EINVAL, "workspace must be 256-byte aligned");
+    if (workspace_bytes < s.grid.bytes)
+        return fail(ECOKV_EWORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, s.grid.bytes);
+    s.Q = static_cast<const char *>(Q_dec);
+    s.Kc = static_cast<const char *>(Kc);
+    s.Vc = static_cast<const char *>(Vc);
+    s.Kt = static_cast<const char *>(tails->K);
+    s.Vt = static_cast<const char *>(tails->V);
+    s.counts = counts;
+    s.offsets = offsets;
+    s.tail_counts = tail_counts;
+    s.O = static_cast<float *>(O);
+    s.lse = lse;
+    s.acc = static_cast<float *>(workspace);
+    s.ms = reinterpret_cast<float2 *>(s.acc + (size_t)(s.grid.np + s.grid.nt) * (size_t)s.grid.qrows * si.D);
+    s.L = si.L;
+    s.Hq = si.Hq;
+    s.Hkv = si.Hkv;
+    s.G = si.G;
+    s.B = si.B;
+    s.N = s.fan[si.B];
+    s.D = si.D;
+    s.max_count = max_count;
+    s.max_tail = max_tail;
+    s.qscale = 1.4426950408889634f / sqrtf((float)si.D);
+    s.nodes = num_nodes;
+    s.bf16 = bf16;
+    a.masks = reinterpret_cast<const unsigned long long *>(masks);
+    a.conts = fan[si.B];
+    const hipError_t e = ecokv::tree_launch(a, bf16, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "ecokv_decode_tree launch");
+    return ECOKV_OK;
+}
+
+int ecokv_commit(int dtype, const ecokv_shape *shape, const ecokv_tails *tails, const int32_t *tail_counts,
+                 int32_t num_nodes, const int32_t *path, const int32_t *accepted, void *stream)
+{
+    ShapeInfo si;
+    memset(&si, 0, sizeof si);
+    int rc = check_heads(shape, &si);
+    if (rc) return rc;
+    if (dtype != ECOKV_BF16 && dtype != ECOKV_F32) return fail(ECOKV_EUNSUPPORTED, "dtype %d", dtype);
+    if (num_nodes < 1 || num_nodes > ECOKV_MAX_NODES)
+        return fail(ECOKV_EINVAL, "num_nodes %d outside [1, %d]", num_nodes, ECOKV_MAX_NODES);
+    ecokv::CommitArgs a;
+    memset(&a, 0, sizeof a);
+    Span tk, tv;
+    if (si.L == 0) return ECOKV_OK;
+    const int es = dtype == ECOKV_BF16 ? 2 : 4;
+    if ((rc = check_tails(tails, si, es, &a.map, &tk, &tv))) return rc;
+    if (overlap(tk, tv)) return fail(ECOKV_EINVAL, "the tails' K and V overlap");
+    if (!tail_counts || !path || !accepted) return fail(ECOKV_EINVAL, "tail_counts, path and accepted must be non-NULL");
+    a.units = (int64_t)si.L * si.Hkv * tails->num_conts;
+    if (a.units == 0) return ECOKV_OK;
+    if (a.units > INT32_MAX / 4) return fail(ECOKV_EINVAL, "too many (layer, KV head, continuation) units");
+    a.K = static_cast<char *>(tails->K);
+    a.V = static_cast<char *>(tails->V);
+    a.tail_counts = tail_counts;
+    a.path = path;
+    a.accepted = accepted;
+    a.Hkv = si.Hkv;
+    a.N = tails->num_conts;
+    a.nodes = num_nodes;
+    a.row_bytes = si.D * es;
+    const hipError_t e = ecokv::commit_launch(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "ecokv_commit launch");
+    return ECOKV_OK;
+}
+
+int ecokv_accumulate(const void *Q_dec, const float *lse, const void *Kc, int dtype, const ecokv_shape *shape,
+                     const int32_t *fan, const int32_t *counts, const int32_t *offsets, int32_t max_count,
+                     const ecokv_tails *tails, const int32_t *tail_counts, int32_t max_tail, int32_t num_nodes,
+                     const int32_t *path, const int32_t *accepted, float decay, const float *mass, const float *tail_mass,
+                     float *mass_out, float *tail_mass_out, void *stream)
+{
+    ShapeInfo si;
+    ecokv::MassArgs a;
+    memset(&a, 0, sizeof a);
+    int rc = check_shape(shape, &si);
+    if (rc) return rc;
+    if (dtype != ECOKV_BF16 && dtype != ECOKV_F32) return fail(ECOKV_EUNSUPPORTED, "dtype %d", dtype);
+    int32_t nodes[ECOKV_MAX_SEQS + 1];
+    if ((rc = check_tree(si, fan, max_count, max_tail, num_nodes, nodes))) return rc;
+    if (!(isfinite(decay) && decay >= 0.f)) return fail(ECOKV_EINVAL, "decay %g", (double)decay);
+    if ((path == nullptr) != (accepted == nullptr)) return fail(ECOKV_EINVAL, "path and accepted: both or neither");
+    if (!path && num_nodes != 1) return fail(ECOKV_EINVAL, "%d queries of a continuation need path and accepted", num_nodes);
+    const int N = fan[si.B];
+    if (si.L == 0 || (max_count == 0 && (max_tail == 0 || N == 0))) return ECOKV_OK;
+    if (N > 0 && (!Q_dec || !lse)) return fail(ECOKV_EINVAL, "Q_dec and lse must be non-NULL");
+    if (max_count > 0 && (!Kc || !counts || !offsets || !mass || !mass_out))
+        return fail(ECOKV_EINVAL, "Kc, counts, offsets, mass and mass_out must be non-NULL");
+    if ((((uintptr_t)Q_dec | (uintptr_t)Kc) & 15u) != 0) return fail(ECOKV_EINVAL, "Q_dec and Kc must be 16-byte aligned");
+    const bool bf16 = dtype == ECOKV_BF16;
+    const bool tailed = max_tail > 0 && N > 0;
+    if (tailed) {
+        Span tk, tv;
+        if ((rc = check_tails(tails, si, bf16 ? 2 : 4, &a.map, &tk, &tv))) return rc;
+        if ((rc = check_tail_counts(tails, N, tail_counts, max_tail))) return rc;
+        if ((rc = check_tail_mass(tails, si, tail_mass, tail_mass_out))) return rc;
+    }
+    a.Q = static_cast<const char *>(Q_dec);
+    a.lse = lse;
+    a.Kc = static_cast<const char *>(Kc);
+    a.Kt = tailed ? static_cast<const char *>(tails->K) : nullptr;
+    a.counts = counts;
+    a.offsets = offsets;
+    a.tail_counts = tail_counts;
+    a.path = path;
+    a.accepted = accepted;
+    a.mass = mass;
+    a.tail_mass = tail_mass;
+    a.mass_out = mass_out;
+    a.tail_mass_out = tail_mass_out;
+    a.L = si.L;
+    a.Hq = si.Hq;
+    a.Hkv = si.Hkv;
+    a.G = si.G;
+    a.B = si.B;
+    a.N = N;
+    a.D = si.D;
+    a.nodes = num_nodes;
+    a.max_count = max_count;
+    a.max_tail = max_tail;
+    a.decay = decay;
+    const double scale = 1.0 / sqrt((double)si.D);
+    a.scale = (float)scale;
+    a.scale_rest = (float)(scale / a.scale - 1.0);
+    for (int s = 0; s <= si.B; ++s) a.fan[s] = fan[s];
+    ecokv::mass_grid((int64_t)si.L * si.Hkv, si.B, tailed ? N : 0, max_count, max_tail, &a.rt, &a.kept_parts, &a.tail_parts,
+                     &a.kept_blocks, &a.tail_blocks);
+    if (a.kept_blocks > INT32_MAX - (1 << 20) || a.tail_blocks > INT32_MAX - (1 << 20) - a.kept_blocks)
+        return fail(ECOKV_EINVAL, "too many parts of kept rows or tails");
+    const hipError_t e = ecokv::mass_launch(a, bf16, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "ecokv_accumulate launch");
+    return ECOKV_OK;
+}
+
+int ecokv_evict_workspace_size(const ecokv_shape *shape, int32_t groups, int32_t max_rows, int32_t keep, size_t *bytes)
+{
+    ShapeInfo si;
+    memset(&si, 0, sizeof si);
+    const int rc = check_heads(shape, &si);
+    if (rc) return rc;
+    if (!bytes) return fail(ECOKV_EINVAL, "bytes is NULL");
+    if (groups < 0) return fail(ECOKV_EINVAL, "groups %d < 0", groups);
+    if (max_rows < 0 || keep < 1) return fail(ECOKV_EINVAL, "max_rows %d < 0 or keep %d < 1", max_rows, keep);
+    *bytes = sizeof(int) * (size_t)si.L * si.Hkv * groups * (size_t)ecokv::evict_plan_words(max_rows, keep);
+    return ECOKV_OK;
+}
+
+int ecokv_evict(void *Kc, void *Vc, int dtype, const ecokv_shape *shape, const int32_t *counts, const int32_t *offsets,
+                int32_t max_count, int32_t limit, int32_t keep, int32_t recent, const float *mass, float *mass_out,
+                int32_t *new_counts, void *workspace, size_t workspace_bytes, void *stream)
+{
+    ShapeInfo si;
+    ecokv::EvictArgs a;
+    memset(&a, 0, sizeof a);
+    int rc = check_shape(shape, &si);
+    if (rc) return rc;
+    if (dtype != ECOKV_BF16 && dtype != ECOKV_F32) return fail(ECOKV_EUNSUPPORTED, "dtype %d", dtype);
+    if ((rc = check_evict(si, si.B, max_count, limit, keep, recent))) return rc;
+    if (si.L == 0) return ECOKV_OK;
+    if (!Kc || !Vc || !counts || !offsets || !mass || !mass_out || !new_counts)
+        return fail(ECOKV_EINVAL, "Kc, Vc, counts, offsets, mass, mass_out and new_counts must be non-NULL");
+    if ((((uintptr_t)Kc | (uintptr_t)Vc) & 15u) != 0) return fail(ECOKV_EINVAL, "Kc and Vc must be 16-byte aligned");
+    a.K = static_cast<char *>(Kc);
+    a.V = static_cast<char *>(Vc);
+    a.counts = counts;
+    a.offsets = offsets;
+    a.max_rows = max_count;
+    return evict_impl(a, si, si.B, dtype, limit, keep, recent, mass, mass_out, new_counts, workspace, workspace_bytes, stream);
+}
+
+int ecokv_evict_tails(int dtype, const ecokv_shape *shape, const ecokv_tails *tails, const int32_t *tail_counts,
+                      int32_t max_tail, int32_t limit, int32_t keep, int32_t recent, const float *tail_mass,
+                      float *tail_mass_out, int32_t *new_counts, void *workspace, size_t workspace_bytes, void *stream)
+{
+    ShapeInfo si;
+    memset(&si, 0, sizeof si);
+    ecokv::EvictArgs a;
+    memset(&a, 0, sizeof a);
+    int rc = check_heads(shape, &si);
+    if (rc) return rc;
+    if (dtype != ECOKV_BF16 && dtype != ECOKV_F32) return fail(ECOKV_EUNSUPPORTED, "dtype %d", dtype);
+    if (si.L == 0) return ECOKV_OK;
+    Span tk, tv;
+    if ((rc = check_tails(tails, si, dtype == ECOKV_BF16 ? 2 : 4, &a.map, &tk, &tv))) return rc;
+    if (overlap(tk, tv)) return fail(ECOKV_EINVAL, "the tails' K and V overlap");
+    if ((rc = check_evict(si, tails->num_conts, max_tail, limit, keep, recent))) return rc;
+    if ((rc = check_tail_counts(tails, tails->num_conts, tail_counts, max_tail))) return rc;
+    if ((rc = check_tail_mass(tails, si, tail_mass, tail_mass_out))) return rc;
+    if (!new_counts) return fail(ECOKV_EINVAL, "new_counts must be non-NULL");
+    if (tails->num_conts == 0) return ECOKV_OK;
+    a.K = static_cast<char *>(tails->K);
+    a.V = static_cast<char *>(tails->V);
+    a.counts = tail_counts;
+    a.tails = 1;
+    a.max_rows = max_tail;
+    return evict_impl(a, si, tails->num_conts, dtype, limit, keep, recent, tail_mass, tail_mass_out, new_counts, workspace,
+                      workspace_bytes, stream);
 }
 
 int ecokv_pyramid_budgets(int num_layers, double total, double beta, int window, int32_t *out)

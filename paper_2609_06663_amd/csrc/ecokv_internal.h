@@ -7,6 +7,8 @@
 #include "ecokv.h"
 #include "ecokv_decode_plan.h"
 #include "ecokv_shared_plan.h"
+#include "ecokv_tree_plan.h"
+#include "ecokv_evict_plan.h"
 
 namespace ecokv {
 
@@ -253,8 +255,69 @@ struct SharedArgs {
     TailMap map;
     SharedGrid grid;
     int fan[ECOKV_MAX_SEQS + 1];
+    // ecokv_decode_tree: the nodes of a continuation's tree and whether O is bf16.
+    // Q, O, N, fan and grid.tile0 are of nodes there, the tails' counts and tables
+    // of continuations.
+    int nodes, bf16;
 };
 hipError_t shared_launch(SharedArgs a, bool bf16, hipStream_t st);
+
+// Attention of trees of drafted tokens: SharedArgs and what their tails' part takes.
+struct TreeArgs {
+    SharedArgs s;
+    const unsigned long long *masks;  // [conts][nodes]
+    int conts;
+    TreeTails tails;
+};
+hipError_t tree_launch(const TreeArgs &a, bool bf16, hipStream_t st);
+
+// Attention weights of the cache's rows.
+struct MassArgs {
+    const char *Q, *Kc, *Kt;
+    const float *lse;
+    const int32_t *counts, *offsets, *tail_counts, *path, *accepted;
+    const float *mass, *tail_mass;
+    float *mass_out, *tail_mass_out;
+    int L, Hq, Hkv, G, B, N, D, nodes;
+    int max_count, max_tail;
+    float decay, scale, scale_rest;   // 1 / sqrt(D) = scale (1 + scale_rest)
+    int rt;                           // 16-row tiles of a wave
+    int kept_parts, tail_parts;       // blocks of a unit, of a tail
+    int64_t kept_blocks, tail_blocks;
+    TailMap map;
+    int fan[ECOKV_MAX_SEQS + 1];
+};
+hipError_t mass_launch(const MassArgs &a, bool bf16, hipStream_t st);
+
+// Accepted rows of trees to the ends of the tails.
+struct CommitArgs {
+    char *K, *V;
+    const int32_t *tail_counts, *path, *accepted;
+    int Hkv, N, nodes, row_bytes;
+    int64_t units;  // L Hkv N
+    TailMap map;
+};
+hipError_t commit_launch(const CommitArgs &a, hipStream_t st);
+
+// Eviction of the rows of least mass.  The plan of a unit in the workspace: kPlanHead
+// words (rows that move, or -1 where none is evicted; rows before), then cap words
+// each of rows that move, their places and their masses.
+struct EvictArgs {
+    char *K, *V;
+    const int32_t *counts, *offsets;
+    int32_t *new_counts;
+    const float *mass;
+    float *mass_out;
+    int *plan;
+    int Hkv, groups, row_bytes, tails;   // groups: prompts, or continuations
+    int max_rows, limit, keep, recent;
+    int cap;
+    int64_t plan_stride;
+    int cols, splits;                    // of the moves: chunks of a row's K and V per block
+    int64_t units;                       // L Hkv groups
+    TailMap map;
+};
+hipError_t evict_launch(EvictArgs a, hipStream_t st);
 
 // The sweeps of ecokv_sweep.hip (every dtype, head_dim and number of window
 // rows): pass 1 or 2 over blocks of a.rpb1 / a.rpb2 keys, a multiple of 128

@@ -1,0 +1,68 @@
+// How ecokv_decode_tree splits a call over blocks: the arithmetic that the
+// workspace size, the grid and the kernels share.  Values only, as
+// ecokv_shared_plan.h, whose prompt parts it takes.
+#pragma once
+
+#include "ecokv_shared_plan.h"
+
+namespace ecokv {
+
+// The tails' part of a call.  A continuation has nodes x G query rows for every
+// (layer, KV head): cut into tiles of wq x rows_q; its tail and the drafted rows
+// behind it into grid.nt parts.  wq = 4: a block takes one tile and one part;
+// wq = 1 (the query rows fit one wave): a wave does.
+struct TreeTails {
+    int wq, tiles;
+    int64_t blocks;
+};
+
+// fan counts nodes (fan[s + 1] - fan[s] of prompt s); conts continuations.
+inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *fan, int conts, int nodes, int max_count,
+                            int max_tail, bool bf16, TreeTails *tails)
+{
+    SharedGrid g{};
+    g.rows_q = g.rows_t = bf16 ? 32 : 16;
+    int64_t most = 0, narrow_tiles = 0, prompts = 0;
+    for (int s = 0; s < B; ++s) {
+        const int64_t m = (int64_t)G * (fan[s + 1] - fan[s]);
+        most = m > most ? m : most;
+        narrow_tiles += (m + g.rows_q - 1) / g.rows_q;
+        prompts += m > 0;
+    }
+    // (as in shared_grid, but with query tiles of one wave or four)
+    const bool narrow = (double)(pairs * narrow_tiles) * max_count * D * (bf16 ? 4 : 8) <= (double)kShNarrow;
+    g.wq = narrow || most <= g.rows_q ? 1 : 4;
+    g.step = g.rows_t * (kShWaves / g.wq);
+    const int qt = g.wq * g.rows_q;
+    for (int s = 0; s < B; ++s) g.tile0[s + 1] = g.tile0[s] + (int)(((int64_t)G * (fan[s + 1] - fan[s]) + qt - 1) / qt);
+    g.tiles = max_count > 0 ? g.tile0[B] : 0;
+    g.qrows = pairs * G * fan[B];
+    g.np = prompt_parts(g, pairs * g.tiles, pairs * prompts, D, max_count, bf16);
+    g.prompt_blocks = pairs * g.tiles * g.np;
+
+    const int rows = max_tail + nodes;
+    tails->wq = nodes * G <= g.rows_q ? 1 : 4;
+    const int tt = tails->wq * g.rows_q;
+    tails->tiles = (nodes * G + tt - 1) / tt;
+    const int64_t have = pairs * conts * tails->tiles;
+    if (tails->wq == 1) {
+        g.tail_step = 2 * g.rows_t;
+        g.nt = tail_parts(g.np == 0, have, rows, g.tail_step);
+        g.tail_waves = have * g.nt;
+        tails->blocks = (g.tail_waves + kShWaves - 1) / kShWaves;
+    } else {
+        g.tail_step = g.rows_t;
+        if (g.np > 0) {
+            const int64_t like = ((int64_t)max_count + g.np - 1) / g.np;  // rows of a prompt's part
+            g.nt = parts_within((rows + like - 1) / like, rows, g.tail_step);
+        } else {
+            g.nt = prompt_parts(g, have, pairs * conts, D, rows, bf16);
+        }
+        g.tail_waves = 0;
+        tails->blocks = have * g.nt;
+    }
+    g.bytes = sizeof(float) * (size_t)(g.np + g.nt) * (size_t)g.qrows * (size_t)(D + 2);
+    return g;
+}
+
+}  // namespace ecokv

@@ -27,7 +27,7 @@ NORM_MINMAX, NORM_WINSOR, NORM_MAD = 0, 1, 2
 RED_EUCLID, RED_STD = 0, 1
 CENTROID_ALL, CENTROID_PREFIX = 0, 1
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BY_PARTS = 0, 1, 2, 3
-MAX_SEQS, MAX_ROWS = 64, 64
+MAX_SEQS, MAX_ROWS, MAX_NODES = 64, 64, 64
 NSTATS = 12
 STAT = dict(lambda_=0, rC=1, rE=2, DE=3, dmin=4, dmax=5, sdmin=6, sdmax=7, imp_mean=8, sbar_mean=9,
             mu_norm2=10, scale=11)
@@ -40,6 +40,8 @@ EXPORTS = ["ecokv_default_params", "ecokv_workspace_size", "ecokv_workspace_stat
            "ecokv_decode_workspace_size", "ecokv_decode",
            "ecokv_rope_freqs", "ecokv_prefill_rope", "ecokv_append", "ecokv_decode_shared_workspace_size",
            "ecokv_decode_shared",
+           "ecokv_tree_masks", "ecokv_decode_tree_workspace_size", "ecokv_decode_tree", "ecokv_commit", "ecokv_accumulate",
+           "ecokv_evict_workspace_size", "ecokv_evict", "ecokv_evict_tails",
            "ecokv_last_error", "ecokv_stage_times"]
 
 
@@ -242,6 +244,16 @@ def _load():
                                                        ctypes.POINTER(ctypes.c_size_t)]
     lib.ecokv_decode_shared.argtypes = [vp, vp, vp, ctypes.c_int, sp, i32p, vp, vp, ctypes.c_int32, tp, vp,
                                         ctypes.c_int32, vp, vp, vp, ctypes.c_size_t, vp]
+    i32, sz = ctypes.c_int32, ctypes.c_size_t
+    lib.ecokv_tree_masks.argtypes = [ctypes.c_int, i32p, ctypes.POINTER(ctypes.c_uint64), i32p]
+    lib.ecokv_decode_tree_workspace_size.argtypes = [sp, i32p, i32, i32, i32, ctypes.POINTER(sz)]
+    lib.ecokv_decode_tree.argtypes = [vp, vp, vp, ctypes.c_int, sp, i32p, vp, vp, i32, tp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
+    lib.ecokv_commit.argtypes = [ctypes.c_int, sp, tp, vp, i32, vp, vp, vp]
+    lib.ecokv_accumulate.argtypes = [vp, vp, vp, ctypes.c_int, sp, i32p, vp, vp, i32, tp, vp, i32, i32, vp, vp, ctypes.c_float,
+                                     vp, vp, vp, vp, vp]
+    lib.ecokv_evict_workspace_size.argtypes = [sp, i32, i32, i32, ctypes.POINTER(sz)]
+    lib.ecokv_evict.argtypes = [vp, vp, ctypes.c_int, sp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+    lib.ecokv_evict_tails.argtypes = [ctypes.c_int, sp, tp, vp, i32, i32, i32, i32, vp, vp, vp, vp, sz, vp]
     lib.ecokv_pyramid_budgets.argtypes = [ctypes.c_int, ctypes.c_double, ctypes.c_double, ctypes.c_int, i32p]
     lib.ecokv_select_workspace_size.argtypes = [sp, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]
     lib.ecokv_select.argtypes = [vp, sp, ctypes.c_int, i32p, vp, vp, vp, vp, ctypes.c_size_t, vp]
@@ -270,7 +282,7 @@ def _ptr(t: Optional[torch.Tensor]):
     return t.data_ptr()
 
 
-_ELEM = {torch.bfloat16: "bf16", torch.float32: "float32", torch.int32: "int32", torch.uint8: "uint8"}
+_ELEM = {torch.bfloat16: "bf16", torch.float32: "float32", torch.int32: "int32", torch.int64: "int64", torch.uint8: "uint8"}
 
 
 def _arg(t: Optional[torch.Tensor], name: str, dtypes, numel: int, device, optional: bool = False):
@@ -788,6 +800,188 @@ def ecokv_decode_shared(Q_dec: torch.Tensor, Kc: Optional[torch.Tensor], Vc: Opt
         workspace = _workspace(None, ecokv_decode_shared_workspace_size(shape, fan, max_count, max_tail), dev, stream)
     _enqueue(lib.ecokv_decode_shared, dev, stream, qp, kp, vp, code, ctypes.byref(c), f, cp, op, max_count, tp, tc, max_tail,
              _fit(O, "O", torch.float32, nq * D, dev), _fit(lse, "lse", torch.float32, nq, dev, True),
+             _fit(workspace, "workspace", torch.uint8, 0, dev), workspace.numel())
+
+
+def ecokv_tree_masks(parents: Sequence[int]):
+    """(masks, depths) as lists: bit j of masks[i] is set if node j is node i or one of
+    its ancestors; parents[i] is an earlier node or -1.  Masks are the signed values
+    that an int64 tensor takes."""
+    p = _flat_ints(parents)
+    n = len(p)
+    arr = (ctypes.c_int32 * max(n, 1))(*[_int32(v, "parents") for v in p])
+    masks, depths = (ctypes.c_uint64 * max(n, 1))(), (ctypes.c_int32 * max(n, 1))()
+    _check(lib.ecokv_tree_masks(n, arr, masks, depths))
+    return [m - (1 << 64) if m >> 63 else m for m in masks], list(depths)
+
+
+def ecokv_decode_tree_workspace_size(shape: Shape, fan: Sequence[int], max_count: int, max_tail: int, num_nodes: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib.ecokv_decode_tree_workspace_size(ctypes.byref(shape.c), _fan(shape, fan), _int32(max_count, "max_count"),
+                                                _int32(max_tail, "max_tail"), _int32(num_nodes, "num_nodes"), ctypes.byref(n)))
+    return n.value
+
+
+def _per_node(t: torch.Tensor, name: str, dtype, conts: int, device) -> int:
+    """Nodes of a contiguous tensor [conts][nodes]."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dim() != 2 or t.shape[0] != conts:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, the call needs ({conts}, nodes)")
+    _fit(t, name, dtype, conts, device)
+    return t.shape[1]
+
+
+def ecokv_decode_tree(Q_dec: torch.Tensor, Kc: Optional[torch.Tensor], Vc: Optional[torch.Tensor], shape: Shape,
+                      fan: Sequence[int], counts: Optional[torch.Tensor], offsets: Optional[torch.Tensor], max_count: int,
+                      tails: Tails, tail_counts: torch.Tensor, max_tail: int, masks: torch.Tensor, O: torch.Tensor,
+                      lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Enqueue ecokv_decode_tree: the drafted tokens of each continuation (masks:
+    int64 [N][nodes], see ecokv_tree_masks) over its prompt's kept rows, its tail and
+    the drafted rows behind it.  Q_dec and O: [L][H_q][N nodes][D] of one element
+    type.  As for ecokv_decode, the caller guarantees that the rows offsets[u] .. +
+    counts[u] lie inside Kc and Vc."""
+    c = shape.c
+    f = _fan(shape, fan)
+    N = f[c.num_seqs]
+    if c.num_layers == 0 or N == 0:
+        return
+    dev, dt, code = _first(Q_dec, "Q_dec")
+    D = c.head_dim
+    M = _per_node(masks, "masks", torch.int64, N, dev)
+    nq = c.num_layers * c.num_q_heads * N * M
+    max_count, max_tail = _int32(max_count, "max_count"), _int32(max_tail, "max_tail")
+    qp = _fit(Q_dec, "Q_dec", dt, nq * D, dev)
+    units = shape.units
+    kp = vp = cp = op = None
+    if max_count > 0:  # (what a bound of 0 leaves unread may be anything)
+        kp, vp = _fit(Kc, "Kc", dt, D, dev), _fit(Vc, "Vc", dt, D, dev)
+        if Kc.numel() % D or Vc.numel() != Kc.numel():
+            raise ValueError("Kc and Vc must hold the same whole number of rows of head_dim elements")
+        cp, op = _fit(counts, "counts", torch.int32, units, dev), _fit(offsets, "offsets", torch.int32, units, dev)
+    if tails is None:
+        raise ValueError("tails is required")
+    if workspace is None:
+        workspace = _workspace(None, ecokv_decode_tree_workspace_size(shape, fan, max_count, max_tail, M), dev, stream)
+    _enqueue(lib.ecokv_decode_tree, dev, stream, qp, kp, vp, code, ctypes.byref(c), f, cp, op, max_count, tails._arg(shape, dt, dev),
+             _fit(tail_counts, "tail_counts", torch.int32, N, dev), max_tail, M, masks.data_ptr(), _fit(O, "O", dt, nq * D, dev),
+             _fit(lse, "lse", torch.float32, nq, dev, True), _fit(workspace, "workspace", torch.uint8, 0, dev), workspace.numel())
+
+
+def ecokv_commit(shape: Shape, tails: Tails, tail_counts: torch.Tensor, path: torch.Tensor, accepted: torch.Tensor,
+                 stream=None) -> None:
+    """Enqueue ecokv_commit: row tail_counts[c] + path[c][k] to row tail_counts[c] + k,
+    k < accepted[c] (path: int32 [N][nodes])."""
+    c = shape.c
+    if c.num_layers == 0:
+        return
+    dev, dt, code = _first(tails.K, "the tails' K")
+    N = tails.table.shape[0]
+    M = _per_node(path, "path", torch.int32, N, dev)
+    if N == 0:
+        return
+    _enqueue(lib.ecokv_commit, dev, stream, code, ctypes.byref(c), tails._arg(shape, dt, dev),
+             _fit(tail_counts, "tail_counts", torch.int32, N, dev), M, path.data_ptr(),
+             _fit(accepted, "accepted", torch.int32, N, dev))
+
+
+def ecokv_accumulate(Q_dec: torch.Tensor, lse: torch.Tensor, Kc: Optional[torch.Tensor], shape: Shape, fan: Sequence[int],
+                     counts: Optional[torch.Tensor], offsets: Optional[torch.Tensor], max_count: int, tails: Optional[Tails],
+                     tail_counts: Optional[torch.Tensor], max_tail: int, mass: Optional[torch.Tensor],
+                     tail_mass: Optional[torch.Tensor], path: Optional[torch.Tensor] = None,
+                     accepted: Optional[torch.Tensor] = None, decay: float = 1.0, mass_out: Optional[torch.Tensor] = None,
+                     tail_mass_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Enqueue ecokv_accumulate: the attention weights of a step added to mass (float32,
+    one per row of Kc) and tail_mass (float32, the tails' K without its last dimension),
+    or written to mass_out and tail_mass_out.  path and accepted: the accepted nodes
+    of trees, as ecokv_commit took them; without them one query of each continuation."""
+    c = shape.c
+    f = _fan(shape, fan)
+    N = f[c.num_seqs]
+    if c.num_layers == 0:
+        return
+    max_count, max_tail = _int32(max_count, "max_count"), _int32(max_tail, "max_tail")
+    dev, dt, code = _first(Q_dec, "Q_dec")
+    if (path is None) != (accepted is None):
+        raise ValueError("path and accepted: both or neither")
+    M = 1 if path is None else _per_node(path, "path", torch.int32, N, dev)
+    D = c.head_dim
+    nq = c.num_layers * c.num_q_heads * N * M
+    kp = cp = op = mp = mo = tp = tc = tm = to = None
+    if max_count > 0:
+        kp = _fit(Kc, "Kc", dt, D, dev)
+        if Kc.numel() % D:
+            raise ValueError("Kc must hold a whole number of rows of head_dim elements")
+        cp, op = (_fit(t, n, torch.int32, shape.units, dev) for t, n in ((counts, "counts"), (offsets, "offsets")))
+        rows = Kc.numel() // D
+        mp = _fit(mass, "mass", torch.float32, rows, dev)
+        mo = mp if mass_out is None else _fit(mass_out, "mass_out", torch.float32, rows, dev)
+    if max_tail > 0 and N > 0:
+        if tails is None:
+            raise ValueError("tails is required")
+        tp, tc = tails._arg(shape, dt, dev), _fit(tail_counts, "tail_counts", torch.int32, N, dev)
+        rows = tails.K.numel() // D
+        tm = _fit(tail_mass, "tail_mass", torch.float32, rows, dev)
+        to = tm if tail_mass_out is None else _fit(tail_mass_out, "tail_mass_out", torch.float32, rows, dev)
+    _enqueue(lib.ecokv_accumulate, dev, stream, _fit(Q_dec, "Q_dec", dt, nq * D, dev), _fit(lse, "lse", torch.float32, nq, dev), kp,
+             code, ctypes.byref(c), f, cp, op, max_count, tp, tc, max_tail, M, None if path is None else path.data_ptr(),
+             _fit(accepted, "accepted", torch.int32, N, dev, True), float(decay), mp, tm, mo, to)
+
+
+def ecokv_evict_workspace_size(shape: Shape, groups: int, max_rows: int, keep: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib.ecokv_evict_workspace_size(ctypes.byref(shape.c), _int32(groups, "groups"), _int32(max_rows, "max_rows"),
+                                          _int32(keep, "keep"), ctypes.byref(n)))
+    return n.value
+
+
+def ecokv_evict(Kc: torch.Tensor, Vc: torch.Tensor, shape: Shape, counts: torch.Tensor, offsets: torch.Tensor, max_count: int,
+                limit: int, keep: int, recent: int, mass: torch.Tensor, new_counts: Optional[torch.Tensor] = None,
+                mass_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Enqueue ecokv_evict: units of more than `limit` rows keep their last `recent`
+    and, of the others, the keep - recent of the largest mass.  new_counts and mass_out:
+    counts and mass themselves where not given.  As for ecokv_decode, the caller
+    guarantees that the rows offsets[u] .. + counts[u] lie inside Kc and Vc."""
+    c = shape.c
+    if c.num_layers == 0:
+        return
+    dev, dt, code = _first(Kc, "Kc")
+    D = c.head_dim
+    max_count, keep = _int32(max_count, "max_count"), _int32(keep, "keep")
+    if Kc.numel() % D or Vc.numel() != Kc.numel():
+        raise ValueError("Kc and Vc must hold the same whole number of rows of head_dim elements")
+    rows, units = Kc.numel() // D, shape.units
+    cp, mp = _fit(counts, "counts", torch.int32, units, dev), _fit(mass, "mass", torch.float32, rows, dev)
+    if workspace is None:
+        workspace = _workspace(None, ecokv_evict_workspace_size(shape, c.num_seqs, max_count, keep), dev, stream)
+    _enqueue(lib.ecokv_evict, dev, stream, _fit(Kc, "Kc", dt, D, dev), _fit(Vc, "Vc", dt, D, dev), code, ctypes.byref(c), cp,
+             _fit(offsets, "offsets", torch.int32, units, dev), max_count, _int32(limit, "limit"), keep, _int32(recent, "recent"), mp,
+             mp if mass_out is None else _fit(mass_out, "mass_out", torch.float32, rows, dev),
+             cp if new_counts is None else _fit(new_counts, "new_counts", torch.int32, units, dev),
+             _fit(workspace, "workspace", torch.uint8, 0, dev), workspace.numel())
+
+
+def ecokv_evict_tails(shape: Shape, tails: Tails, tail_counts: torch.Tensor, max_tail: int, limit: int, keep: int, recent: int,
+                      tail_mass: torch.Tensor, new_counts: Optional[torch.Tensor] = None,
+                      mass_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Enqueue ecokv_evict_tails: the same for tails of more than `limit` rows.
+    tail_mass: float32, the tails' K without its last dimension."""
+    c = shape.c
+    if c.num_layers == 0:
+        return
+    dev, dt, code = _first(tails.K, "the tails' K")
+    N = tails.table.shape[0]
+    if N == 0:
+        return
+    max_tail, keep = _int32(max_tail, "max_tail"), _int32(keep, "keep")
+    tp = tails._arg(shape, dt, dev)
+    rows = tails.K.numel() // c.head_dim
+    cp, mp = _fit(tail_counts, "tail_counts", torch.int32, N, dev), _fit(tail_mass, "tail_mass", torch.float32, rows, dev)
+    if workspace is None:
+        workspace = _workspace(None, ecokv_evict_workspace_size(shape, N, max_tail, keep), dev, stream)
+    _enqueue(lib.ecokv_evict_tails, dev, stream, code, ctypes.byref(c), tp, cp, max_tail, _int32(limit, "limit"), keep,
+             _int32(recent, "recent"), mp, mp if mass_out is None else _fit(mass_out, "mass_out", torch.float32, rows, dev),
+             cp if new_counts is None else _fit(new_counts, "new_counts", torch.int32, N, dev),
              _fit(workspace, "workspace", torch.uint8, 0, dev), workspace.numel())
 
 
