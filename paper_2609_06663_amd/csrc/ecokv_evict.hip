@@ -120,7 +120,191 @@ __device__ __forceinline__ int block_rank(bool f, int *waves, int &total)
     return before + __popcll(m & ((1ull << lane) - 1));
 }
 
-__global__ __launch_bounds__(kPlanThreads) void k_evict_plan(EvictArgs a)
+// What a unit's block finds out before it selects: whether the unit is left alone, its
+// rows, where its plan is.
+struct EvictPlan {
+    EvictUnit x;
+    int n, heavy, old;
+    int *head, *src, *dst;
+    float *mv;
+};
+__device__ __forceinline__ EvictPlan evict_plan(const EvictArgs &a, uint32_t u)
+{
+    EvictPlan p;
+    p.x = evict_unit(a, u);
+    p.n = uniform_i32(a.tails ? a.counts[p.x.g] : a.counts[u]);
+    p.heavy = a.keep - a.recent;
+    p.old = p.n - a.recent;
+    p.head = a.plan + (int64_t)u * a.plan_stride;
+    p.src = p.head + kPlanHead;
+    p.dst = p.src + a.cap;
+    p.mv = reinterpret_cast<float *>(p.dst + a.cap);
+    return p;
+}
+// Whether this thread sees a row of the tail that has no page.
+template <int T>
+__device__ __forceinline__ int evict_lost(const EvictArgs &a, const EvictPlan &p)
+{
+    int lost = 0;
+    if (a.tails) {
+        const int pages = (p.n + (1 << a.map.shift) - 1) >> a.map.shift;
+        for (int i = threadIdx.x; i < pages; i += T) lost |= tail_page(a.map, p.x.g, i << a.map.shift) < 0;
+    }
+    return lost;
+}
+// Not past the limit: nothing goes, another buffer gets the masses as they are.
+template <int T>
+__device__ __forceinline__ void evict_none(const EvictArgs &a, const EvictPlan &p)
+{
+    if (a.mass_out != a.mass)
+        for (int r = threadIdx.x; r < p.n; r += T) {
+            const int64_t at = evict_at(a, p.x, r);
+            a.mass_out[at] = a.mass[at];
+        }
+}
+// The masses of the rows that move, after the lists.
+template <int T>
+__device__ __forceinline__ void evict_masses(const EvictArgs &a, const EvictPlan &p, int movers)
+{
+    __syncthreads();
+    for (int i = threadIdx.x; i < movers; i += T) a.mass_out[evict_at(a, p.x, p.dst[i])] = p.mv[i];
+    for (int r0 = 0; r0 < a.recent; r0 += T) {
+        const int r = r0 + (int)threadIdx.x;
+        const float m = r < a.recent ? a.mass[evict_at(a, p.x, p.old + r)] : 0.f;
+        __syncthreads();  // (a place may be a row that another thread has yet to read)
+        if (r < a.recent) a.mass_out[evict_at(a, p.x, p.heavy + r)] = m;
+    }
+    if (threadIdx.x == 0) p.head[0] = movers;
+}
+
+// A unit of at most T KPT rows: thread t has rows t, t + T, .., their keys in
+// registers.  The key of the heavy-th heaviest row bit by bit from the top, a count of
+// the block's keys for each, until the keys from it on are as many as stay (then they
+// are those, whatever its other bits); equal keys are ranked only where some of them go.
+template <int T, int KPT>
+__global__ __launch_bounds__(T) void k_evict_plan(EvictArgs a)
+{
+    constexpr int W = T / kWave, TAB = KPT * W;
+    __shared__ int count[2][W], tab[2][TAB], total[2];
+    const uint32_t u = blockIdx.z * (uint32_t)kGridX + blockIdx.x;
+    if (u >= (uint32_t)a.units) return;
+    const int t = threadIdx.x, lane = t & 63, wv = uniform_i32(t >> 6);
+    const EvictPlan p = evict_plan(a, u);
+    const int n = p.n, heavy = p.heavy, old = p.old;
+    if (t == 0) {
+        p.head[0] = -1;
+        p.head[1] = n;
+    }
+    if (n < 0 || n > a.max_rows) return;
+    if (n <= a.limit) {
+        if (__syncthreads_or(evict_lost<T>(a, p))) return;
+        evict_none<T>(a, p);
+        return;
+    }
+    int64_t at[KPT];
+    uint32_t key[KPT];
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) at[i] = i * T < old ? evict_at(a, p.x, min(i * T + t, old - 1)) : 0;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) key[i] = i * T + t < old ? score_key(a.mass[at[i]]) : 0u;
+    if (__syncthreads_or(evict_lost<T>(a, p))) return;
+
+    const auto keys = [&](auto in) {  // of the wave for which in(key) holds
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < KPT; ++i)
+            if (i * T < old) c += __popcll(__builtin_amdgcn_ballot_w64(in(key[i])));
+        return c;
+    };
+    int turn = 0;
+    const auto of_block = [&](int c) {
+        if (W == 1) return c;
+        if (lane == 0) count[turn][wv] = c;
+        lds_barrier();
+        c = 0;
+#pragma unroll
+        for (int i = 0; i < W; ++i) c += count[turn][i];
+        turn ^= 1;
+        return uniform_i32(c);
+    };
+    uint32_t least = 0;  // the keys from here on are `many`
+    int many = old, need = INT32_MAX;
+    if (heavy > 0) {
+#pragma unroll 1
+        for (uint32_t bit = 1u << 31; bit && many != heavy; bit >>= 1) {
+            const uint32_t cand = least | bit;
+            const int c = of_block(keys([&](uint32_t k) { return k >= cand; }));
+            if (c >= heavy) least = cand, many = c;
+        }
+        if (many != heavy) need = heavy - of_block(keys([&](uint32_t k) { return k > least; }));
+    }
+
+    // ranks in the rows' order: the sums before each wave's 64 rows, then before the lane
+    const auto ranks = [&](int k) {
+        lds_barrier();
+        if (wv == 0) {
+            int before = 0;
+            for (int b = 0; b < TAB; b += kWave) {
+                const int v = b + lane < TAB ? tab[k][b + lane] : 0;
+                const int end = (int)wave_incl_scan((uint32_t)v);
+                if (b + lane < TAB) tab[k][b + lane] = before + end - v;
+                before += __builtin_amdgcn_readlane(end, 63);
+            }
+            if (lane == 0) total[k] = before;
+        }
+    };
+    const auto below = [&](unsigned long long m) { return __popcll(m & ((1ull << lane) - 1)); };
+    unsigned stays = 0;
+    if (need != INT32_MAX) {
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            const int c = i * T < old ? __popcll(__builtin_amdgcn_ballot_w64(i * T + t < old && key[i] == least)) : 0;
+            if (lane == 0) tab[0][i * W + wv] = c;
+        }
+        ranks(0);
+        lds_barrier();
+    }
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        const bool there = i * T + t < old && heavy > 0;
+        bool s = there && key[i] >= least;
+        if (need != INT32_MAX) {
+            const bool same = there && key[i] == least;
+            const int rank = tab[0][i * W + wv] + below(__builtin_amdgcn_ballot_w64(same));
+            s = s && (!same || rank < need);
+        }
+        stays |= (unsigned)s << i;
+    }
+    if (need != INT32_MAX) lds_barrier();  // (tab is free again)
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        const bool s = (stays >> i) & 1u, low = i * T + t < heavy;
+        const int h = __popcll(__builtin_amdgcn_ballot_w64(low && !s)), m = __popcll(__builtin_amdgcn_ballot_w64(!low && s));
+        if (lane == 0) tab[0][i * W + wv] = h, tab[1][i * W + wv] = m;
+    }
+    ranks(0);
+    ranks(1);
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        if (i * T >= old) continue;
+        const int r = i * T + t;
+        const bool s = (stays >> i) & 1u, low = r < heavy;
+        const unsigned long long h = __builtin_amdgcn_ballot_w64(low && !s), m = __builtin_amdgcn_ballot_w64(!low && s);
+        if (low && !s) p.dst[tab[0][i * W + wv] + below(h)] = r;
+        if (s && !low) {
+            const int j = tab[1][i * W + wv] + below(m);
+            p.src[j] = r;
+            p.mv[j] = a.mass[at[i]];
+        }
+        if (s && low && a.mass_out != a.mass) a.mass_out[at[i]] = a.mass[at[i]];
+    }
+    evict_masses<T>(a, p, total[1]);
+}
+
+// The same for units of any number of rows, whose masses are read again for every
+// digit of the key.
+__global__ __launch_bounds__(kPlanThreads) void k_evict_plan_long(EvictArgs a)
 {
     __shared__ uint32_t hist[2048];
     __shared__ int waves[kPlanWaves];
@@ -128,32 +312,18 @@ __global__ __launch_bounds__(kPlanThreads) void k_evict_plan(EvictArgs a)
     const uint32_t u = blockIdx.z * (uint32_t)kGridX + blockIdx.x;
     if (u >= (uint32_t)a.units) return;
     const int t = threadIdx.x;
-    const EvictUnit x = evict_unit(a, u);
-    const int n = uniform_i32(a.tails ? a.counts[x.g] : a.counts[u]);
-    int *const head = a.plan + (int64_t)u * a.plan_stride;
-    int *const src = head + kPlanHead, *const dst = src + a.cap;
-    float *const mv = reinterpret_cast<float *>(dst + a.cap);
-    bool out = n < 0 || n > a.max_rows;
-    if (a.tails && !out) {
-        int lost = 0;
-        const int pages = (n + (1 << a.map.shift) - 1) >> a.map.shift;
-        for (int p = t; p < pages; p += kPlanThreads) lost |= tail_page(a.map, x.g, p << a.map.shift) < 0;
-        out = __syncthreads_or(lost);
-    }
+    const EvictPlan p = evict_plan(a, u);
+    const EvictUnit &x = p.x;
+    const int n = p.n, heavy = p.heavy, old = p.old;
     if (t == 0) {
-        head[0] = out || n <= a.limit ? -1 : 0;
-        head[1] = n;
+        p.head[0] = -1;
+        p.head[1] = n;
     }
-    if (out) return;
-    if (n <= a.limit) {  // nothing goes; another buffer gets the masses as they are
-        if (a.mass_out != a.mass)
-            for (int r = t; r < n; r += kPlanThreads) {
-                const int64_t at = evict_at(a, x, r);
-                a.mass_out[at] = a.mass[at];
-            }
+    if (n < 0 || n > a.max_rows || __syncthreads_or(evict_lost<kPlanThreads>(a, p))) return;
+    if (n <= a.limit) {
+        evict_none<kPlanThreads>(a, p);
         return;
     }
-    const int heavy = a.keep - a.recent, old = n - a.recent;
     // the key of the heavy-th heaviest of the older rows, digit by digit; `need` rows of it stay
     uint32_t key = 0, need = (uint32_t)heavy;
     if (heavy > 0) {
@@ -202,19 +372,11 @@ __global__ __launch_bounds__(kPlanThreads) void k_evict_plan(EvictArgs a)
         holes += total;
         const int j = movers + block_rank(mover, waves, total);
         movers += total;
-        if (hole) dst[i] = r;
-        if (mover) src[j] = r, mv[j] = m;
+        if (hole) p.dst[i] = r;
+        if (mover) p.src[j] = r, p.mv[j] = m;
         if (stays && r < heavy && a.mass_out != a.mass) a.mass_out[evict_at(a, x, r)] = m;
     }
-    __syncthreads();
-    for (int i = t; i < movers; i += kPlanThreads) a.mass_out[evict_at(a, x, dst[i])] = mv[i];
-    for (int r0 = 0; r0 < a.recent; r0 += kPlanThreads) {
-        const int r = r0 + t;
-        const float m = r < a.recent ? a.mass[evict_at(a, x, old + r)] : 0.f;
-        __syncthreads();  // (a place may be a row that another thread has yet to read)
-        if (r < a.recent) a.mass_out[evict_at(a, x, heavy + r)] = m;
-    }
-    if (t == 0) head[0] = movers;
+    evict_masses<kPlanThreads>(a, p, movers);
 }
 
 // A block moves the chunks [c0, c0 + cols) of 16 bytes of a unit's rows, K's and V's
@@ -239,24 +401,48 @@ __global__ __launch_bounds__(kMoveThreads) void k_evict_move(EvictArgs a)
     char *const pool = (chunk < S ? a.K : a.V) + 16 * (chunk % S);
     const auto row = [&](int r) { return reinterpret_cast<u32x4e *>(pool + evict_at(a, x, r) * a.row_bytes); };
     constexpr int U = 4;
-    for (int i = 0; i < moves; i += U * per) {
-        u32x4e v[U];
+    const int step = U * per;
+    u32x4e v[U], w[U];
+    // the rows that fill free places; their numbers are read a step ahead
+    const auto number = [&](const int *list, int i, int (&r)[U]) {
 #pragma unroll
-        for (int j = 0; j < U; ++j) v[j] = *row(src[min(i + j * per + mine, moves - 1)]);
+        for (int j = 0; j < U; ++j) r[j] = list[max(min(i + j * per + mine, moves - 1), 0)];
+    };
+    int from[U], to[U], from2[U], to2[U];
+    if (moves > 0) number(src, 0, from), number(dst, 0, to);
+    for (int i = 0; i < moves; i += step) {
 #pragma unroll
-        for (int j = 0; j < U; ++j)
-            if (i + j * per + mine < moves) *row(dst[i + j * per + mine]) = v[j];
+        for (int j = 0; j < U; ++j) v[j] = *row(from[j]);
+        number(src, i + step, from2), number(dst, i + step, to2);
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            if (i + j * per + mine < moves) *row(to[j]) = v[j];
+            from[j] = from2[j], to[j] = to2[j];
+        }
     }
     __syncthreads();  // (a newest row's place may be one that moved from there)
+    // The newest rows, a step's loads ahead of the stores of the one before: a place is
+    // below every row of the steps after, and where it may be a row of its own step the
+    // block waits for that step's loads.
     const int heavy = a.keep - a.recent, old = n - a.recent;
-    for (int i = 0; i < a.recent; i += U * per) {
-        u32x4e v[U];
+    const bool apart = n - a.keep >= a.recent;
+    const auto load = [&](u32x4e (&x)[U], int i) {
 #pragma unroll
-        for (int j = 0; j < U; ++j) v[j] = *row(old + min(i + j * per + mine, a.recent - 1));
-        __syncthreads();
+        for (int j = 0; j < U; ++j) x[j] = *row(old + max(min(i + j * per + mine, a.recent - 1), 0));
+    };
+    if (a.recent > 0) load(v, 0);
+    for (int i = 0; i < a.recent; i += step) {
+        if (!apart) {
 #pragma unroll
-        for (int j = 0; j < U; ++j)
+            for (int j = 0; j < U; ++j) asm volatile("" ::"v"(v[j]));  // (loaded)
+            lds_barrier();
+        }
+        if (i + step < a.recent) load(w, i + step);
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
             if (i + j * per + mine < a.recent) *row(heavy + i + j * per + mine) = v[j];
+            v[j] = w[j];
+        }
     }
 }
 
@@ -265,11 +451,17 @@ hipError_t evict_launch(EvictArgs a, hipStream_t st)
     const auto grid = [](int64_t n) {
         return dim3((unsigned)(n < kGridX ? n : kGridX), 1, (unsigned)((n + kGridX - 1) / kGridX));
     };
-    ECOKV_TIMED("evict_plan", st, hipLaunchKernelGGL(k_evict_plan, grid(a.units), dim3(kPlanThreads), 0, st, a));
+    const dim3 units = grid(a.units);
+    if (a.max_rows <= 2048) ECOKV_TIMED("evict_plan", st, hipLaunchKernelGGL((k_evict_plan<256, 8>), units, dim3(256), 0, st, a));
+    else if (a.max_rows <= 8192) ECOKV_TIMED("evict_plan", st, hipLaunchKernelGGL((k_evict_plan<1024, 8>), units, dim3(1024), 0, st, a));
+    else ECOKV_TIMED("evict_plan", st, hipLaunchKernelGGL(k_evict_plan_long, units, dim3(kPlanThreads), 0, st, a));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    a.cols = a.row_bytes / 16;
-    a.splits = 2;
+    // chunks of a row's K and V that a block moves: all of them, or fewer where that
+    // leaves fewer than four blocks for each compute unit, down to 128 bytes
+    a.cols = a.row_bytes / 8;
+    while (a.cols > 8 && a.units * (a.row_bytes / 8 / a.cols) < 4 * kShBlocks) a.cols /= 2;
+    a.splits = a.row_bytes / 8 / a.cols;
     ECOKV_TIMED("evict_move", st, hipLaunchKernelGGL(k_evict_move, grid(a.units * a.splits), dim3(kMoveThreads), 0, st, a));
     return hipGetLastError();
 }
