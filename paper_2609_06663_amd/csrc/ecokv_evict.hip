@@ -102,6 +102,12 @@ __device__ __forceinline__ int64_t evict_at(const EvictArgs &a, const EvictUnit 
     return tail_row(a.map, a.Hkv, x.l, x.h, max(tail_page(a.map, x.g, r), 0), r);
 }
 
+// Set bits of a wave's mask below this lane's.
+__device__ __forceinline__ int lanes_below(unsigned long long m)
+{
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
+}
+
 // Exclusive sums over the block of 0 or 1 of every thread; `total` of all.
 __device__ __forceinline__ int block_rank(bool f, int *waves, int &total)
 {
@@ -117,7 +123,7 @@ __device__ __forceinline__ int block_rank(bool f, int *waves, int &total)
         before += i < wv ? waves[i] : 0;
         total += waves[i];
     }
-    return before + __popcll(m & ((1ull << lane) - 1));
+    return before + lanes_below(m);
 }
 
 // What a unit's block finds out before it selects: whether the unit is left alone, its
@@ -126,7 +132,6 @@ struct EvictPlan {
     EvictUnit x;
     int n, heavy, old;
     int *head, *src, *dst;
-    float *mv;
 };
 __device__ __forceinline__ EvictPlan evict_plan(const EvictArgs &a, uint32_t u)
 {
@@ -138,7 +143,6 @@ __device__ __forceinline__ EvictPlan evict_plan(const EvictArgs &a, uint32_t u)
     p.head = a.plan + (int64_t)u * a.plan_stride;
     p.src = p.head + kPlanHead;
     p.dst = p.src + a.cap;
-    p.mv = reinterpret_cast<float *>(p.dst + a.cap);
     return p;
 }
 // Whether this thread sees a row of the tail that has no page.
@@ -162,30 +166,49 @@ __device__ __forceinline__ void evict_none(const EvictArgs &a, const EvictPlan &
             a.mass_out[at] = a.mass[at];
         }
 }
-// The masses of the rows that move, after the lists.
+// From the top digit of a histogram of 2048 down: the first at which the keys so far
+// reach `need`; pick: that digit, and how many of its keys are needed.  All T threads.
 template <int T>
-__device__ __forceinline__ void evict_masses(const EvictArgs &a, const EvictPlan &p, int movers)
+__device__ __forceinline__ void pick_digit(const uint32_t *hist, uint32_t need, uint32_t *sums, uint32_t *pick)
 {
-    __syncthreads();
-    for (int i = threadIdx.x; i < movers; i += T) a.mass_out[evict_at(a, p.x, p.dst[i])] = p.mv[i];
-    for (int r0 = 0; r0 < a.recent; r0 += T) {
-        const int r = r0 + (int)threadIdx.x;
-        const float m = r < a.recent ? a.mass[evict_at(a, p.x, p.old + r)] : 0.f;
-        __syncthreads();  // (a place may be a row that another thread has yet to read)
-        if (r < a.recent) a.mass_out[evict_at(a, p.x, p.heavy + r)] = m;
+    constexpr int EACH = 2048 / T, W = T / kWave;
+    const int t = threadIdx.x, lane = t & 63, wv = t >> 6, low = (T - 1 - t) * EACH;
+    uint32_t h[EACH], sum = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) sum += h[i] = hist[low + i];
+    uint32_t end = wave_incl_scan(sum);
+    if (lane == 63) sums[wv] = end;
+    lds_barrier();
+#pragma unroll
+    for (int i = 0; i < W; ++i) end += i < wv ? sums[i] : 0;
+    if (end - sum < need && need <= end) {
+        uint32_t left = need - (end - sum);
+        int d = 0;
+#pragma unroll
+        for (int i = EACH - 1; i >= 0; --i) {
+            if (d == 0 && left <= h[i]) d = i + 1;
+            left -= d == 0 ? h[i] : 0;
+        }
+        pick[0] = (uint32_t)(low + d - 1);
+        pick[1] = left;
     }
-    if (threadIdx.x == 0) p.head[0] = movers;
+    lds_barrier();
 }
 
 // A unit of at most T KPT rows: thread t has rows t, t + T, .., their keys in
-// registers.  The key of the heavy-th heaviest row bit by bit from the top, a count of
-// the block's keys for each, until the keys from it on are as many as stay (then they
-// are those, whatever its other bits); equal keys are ranked only where some of them go.
+// registers.  The key of the heavy-th heaviest row digit by digit (11, 11 and 10 bits)
+// by histograms in LDS, until its digit has no more than kEvictFew keys: then one wave
+// takes these and finds it bit by bit.  (By bits of all keys from the top, with the block
+// counting for each of them, the selection took 11 and 12 of 31 and 22 us: 1792 units of
+// 1152 rows, 160 of 5600.)
+constexpr int kEvictFew = 256;
 template <int T, int KPT>
 __global__ __launch_bounds__(T) void k_evict_plan(EvictArgs a)
 {
     constexpr int W = T / kWave, TAB = KPT * W;
-    __shared__ int count[2][W], tab[2][TAB], total[2];
+    __shared__ __align__(16) uint32_t hist[2048];
+    __shared__ uint32_t sums[W], pick[3], few[kEvictFew];
+    __shared__ int tab[2][TAB];
     const uint32_t u = blockIdx.z * (uint32_t)kGridX + blockIdx.x;
     if (u >= (uint32_t)a.units) return;
     const int t = threadIdx.x, lane = t & 63, wv = uniform_i32(t >> 6);
@@ -201,105 +224,129 @@ __global__ __launch_bounds__(T) void k_evict_plan(EvictArgs a)
         evict_none<T>(a, p);
         return;
     }
-    int64_t at[KPT];
     uint32_t key[KPT];
+    {
+        int64_t at[KPT];
 #pragma unroll
-    for (int i = 0; i < KPT; ++i) at[i] = i * T < old ? evict_at(a, p.x, min(i * T + t, old - 1)) : 0;
+        for (int i = 0; i < KPT; ++i) at[i] = i * T < old ? evict_at(a, p.x, min(i * T + t, old - 1)) : 0;
 #pragma unroll
-    for (int i = 0; i < KPT; ++i) key[i] = i * T + t < old ? score_key(a.mass[at[i]]) : 0u;
+        for (int i = 0; i < KPT; ++i) key[i] = i * T + t < old ? score_key(a.mass[at[i]]) : 0u;
+    }
+    for (int i = t; i < 2048; i += T) hist[i] = 0;
+    if (t == 0) pick[2] = 0;
     if (__syncthreads_or(evict_lost<T>(a, p))) return;
 
-    const auto keys = [&](auto in) {  // of the wave for which in(key) holds
-        int c = 0;
-#pragma unroll
-        for (int i = 0; i < KPT; ++i)
-            if (i * T < old) c += __popcll(__builtin_amdgcn_ballot_w64(in(key[i])));
-        return c;
-    };
-    int turn = 0;
-    const auto of_block = [&](int c) {
-        if (W == 1) return c;
-        if (lane == 0) count[turn][wv] = c;
-        lds_barrier();
-        c = 0;
-#pragma unroll
-        for (int i = 0; i < W; ++i) c += count[turn][i];
-        turn ^= 1;
-        return uniform_i32(c);
-    };
-    uint32_t least = 0;  // the keys from here on are `many`
-    int many = old, need = INT32_MAX;
+    uint32_t least = 0, need = (uint32_t)heavy, equal = 0;  // the key, how many equal to it stay, how many there are
     if (heavy > 0) {
 #pragma unroll 1
-        for (uint32_t bit = 1u << 31; bit && many != heavy; bit >>= 1) {
-            const uint32_t cand = least | bit;
-            const int c = of_block(keys([&](uint32_t k) { return k >= cand; }));
-            if (c >= heavy) least = cand, many = c;
+        for (int d = 0; d < 3; ++d) {
+            const int shift = d == 0 ? 21 : d == 1 ? 10 : 0, bits = d == 2 ? 10 : 11;
+            const auto among = [&](uint32_t k) { return d == 0 || (k >> (shift + bits)) == (least >> (shift + bits)); };
+#pragma unroll
+            for (int i = 0; i < KPT; ++i)
+                if (i * T + t < old && among(key[i])) atomicAdd(&hist[(key[i] >> shift) & ((1u << bits) - 1)], 1u);
+            __syncthreads();
+            pick_digit<T>(hist, need, sums, pick);
+            least |= pick[0] << shift;
+            need = pick[1];
+            const uint32_t many = hist[pick[0]];
+            if (d == 2) {
+                equal = many;
+                break;
+            }
+            if (many <= (uint32_t)kEvictFew) {
+                // those that share the digits so far
+#pragma unroll
+                for (int i = 0; i < KPT; ++i)
+                    if (i * T + t < old && (key[i] >> shift) == (least >> shift)) few[atomicAdd(&pick[2], 1u)] = key[i];
+                __syncthreads();
+                if (wv == 0) {
+                    uint32_t mine[kEvictFew / kWave], k = least;
+#pragma unroll
+                    for (int i = 0; i < kEvictFew / kWave; ++i) mine[i] = kWave * i + lane < (int)many ? few[kWave * i + lane] : 0u;
+                    for (uint32_t bit = 1u << (shift - 1); bit; bit >>= 1) {
+                        uint32_t c = 0;
+#pragma unroll
+                        for (int i = 0; i < kEvictFew / kWave; ++i) c += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(mine[i] >= (k | bit)));
+                        if (c >= need) k |= bit;
+                    }
+                    uint32_t above = 0, same = 0;
+#pragma unroll
+                    for (int i = 0; i < kEvictFew / kWave; ++i) {
+                        above += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(mine[i] > k));
+                        same += (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(mine[i] == k && kWave * i + lane < (int)many));
+                    }
+                    if (lane == 0) pick[0] = k, pick[1] = need - above, pick[2] = same;
+                }
+                __syncthreads();
+                least = pick[0];
+                need = pick[1];
+                equal = pick[2];
+                break;
+            }
+            __syncthreads();  // (every thread has read hist)
+            for (int i = t; i < 2048; i += T) hist[i] = 0;
+            __syncthreads();
         }
-        if (many != heavy) need = heavy - of_block(keys([&](uint32_t k) { return k > least; }));
     }
 
-    // ranks in the rows' order: the sums before each wave's 64 rows, then before the lane
-    const auto ranks = [&](int k) {
+    // sums before each wave's 64 rows, of table k by wave k
+    const auto before = [&](int tables) {
         lds_barrier();
-        if (wv == 0) {
-            int before = 0;
+        if (wv < tables) {
+            int sum = 0;
             for (int b = 0; b < TAB; b += kWave) {
-                const int v = b + lane < TAB ? tab[k][b + lane] : 0;
+                const int v = b + lane < TAB ? tab[wv][b + lane] : 0;
                 const int end = (int)wave_incl_scan((uint32_t)v);
-                if (b + lane < TAB) tab[k][b + lane] = before + end - v;
-                before += __builtin_amdgcn_readlane(end, 63);
+                if (b + lane < TAB) tab[wv][b + lane] = sum + end - v;
+                sum += __builtin_amdgcn_readlane(end, 63);
             }
-            if (lane == 0) total[k] = before;
+            if (lane == 0) sums[wv] = (uint32_t)sum;
         }
+        lds_barrier();
     };
-    const auto below = [&](unsigned long long m) { return __popcll(m & ((1ull << lane) - 1)); };
+    // Which rows stay: heavier ones, and of the equal ones the first `need` in the rows'
+    // order.
     unsigned stays = 0;
-    if (need != INT32_MAX) {
+#pragma unroll
+    for (int i = 0; i < KPT; ++i)
+        if (i * T < old) stays |= (unsigned)(i * T + t < old && heavy > 0 && key[i] >= least) << i;
+    if (equal > need) {
 #pragma unroll
         for (int i = 0; i < KPT; ++i) {
-            const int c = i * T < old ? __popcll(__builtin_amdgcn_ballot_w64(i * T + t < old && key[i] == least)) : 0;
+            const int c = __popcll(__builtin_amdgcn_ballot_w64((stays >> i) & (unsigned)(key[i] == least)));
             if (lane == 0) tab[0][i * W + wv] = c;
         }
-        ranks(0);
-        lds_barrier();
-    }
+        before(1);
 #pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-        const bool there = i * T + t < old && heavy > 0;
-        bool s = there && key[i] >= least;
-        if (need != INT32_MAX) {
-            const bool same = there && key[i] == least;
-            const int rank = tab[0][i * W + wv] + below(__builtin_amdgcn_ballot_w64(same));
-            s = s && (!same || rank < need);
+        for (int i = 0; i < KPT; ++i) {
+            const bool s = (stays >> i) & (unsigned)(key[i] == least);
+            if (s && (uint32_t)(tab[0][i * W + wv] + lanes_below(__builtin_amdgcn_ballot_w64(s))) >= need) stays &= ~(1u << i);
         }
-        stays |= (unsigned)s << i;
+        lds_barrier();  // (tab is free again)
     }
-    if (need != INT32_MAX) lds_barrier();  // (tab is free again)
+    // the places that are free (rows below `heavy` that go), and the rows that fill them
+    // (from there on that stay)
+    const auto lows = [&](int i) {
+        const int d = heavy - (i * T + wv * kWave);
+        return d >= 64 ? ~0ull : d > 0 ? (1ull << d) - 1 : 0ull;
+    };
+    unsigned long long odd[KPT];
 #pragma unroll
     for (int i = 0; i < KPT; ++i) {
-        const bool s = (stays >> i) & 1u, low = i * T + t < heavy;
-        const int h = __popcll(__builtin_amdgcn_ballot_w64(low && !s)), m = __popcll(__builtin_amdgcn_ballot_w64(!low && s));
-        if (lane == 0) tab[0][i * W + wv] = h, tab[1][i * W + wv] = m;
+        odd[i] = i * T < old ? __builtin_amdgcn_ballot_w64((stays >> i) & 1u) ^ lows(i) : 0;
+        if (lane == 0) tab[0][i * W + wv] = __popcll(odd[i] & lows(i)), tab[1][i * W + wv] = __popcll(odd[i] & ~lows(i));
     }
-    ranks(0);
-    ranks(1);
-    lds_barrier();
+    before(2);
 #pragma unroll
     for (int i = 0; i < KPT; ++i) {
         if (i * T >= old) continue;
-        const int r = i * T + t;
-        const bool s = (stays >> i) & 1u, low = r < heavy;
-        const unsigned long long h = __builtin_amdgcn_ballot_w64(low && !s), m = __builtin_amdgcn_ballot_w64(!low && s);
-        if (low && !s) p.dst[tab[0][i * W + wv] + below(h)] = r;
-        if (s && !low) {
-            const int j = tab[1][i * W + wv] + below(m);
-            p.src[j] = r;
-            p.mv[j] = a.mass[at[i]];
-        }
-        if (s && low && a.mass_out != a.mass) a.mass_out[at[i]] = a.mass[at[i]];
+        const bool low = i * T + t < heavy;
+        if (!((odd[i] >> lane) & 1)) continue;
+        const int at = tab[low ? 0 : 1][i * W + wv] + lanes_below(odd[i] & (low ? lows(i) : ~lows(i)));
+        (low ? p.dst : p.src)[at] = i * T + t;
     }
-    evict_masses<T>(a, p, total[1]);
+    if (t == 0) p.head[0] = (int)sums[1];
 }
 
 // The same for units of any number of rows, whose masses are read again for every
@@ -360,8 +407,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_evict_plan_long(EvictArgs a)
     int equal = 0, holes = 0, movers = 0;
     for (int r0 = 0; r0 < old; r0 += kPlanThreads) {
         const int r = r0 + t;
-        const float m = r < old ? a.mass[evict_at(a, x, r)] : 0.f;
-        const uint32_t q = score_key(m);
+        const uint32_t q = score_key(r < old ? a.mass[evict_at(a, x, r)] : 0.f);
         int total;
         const bool same = r < old && heavy > 0 && q == key;
         const int rank = equal + block_rank(same, waves, total);
@@ -373,29 +419,57 @@ __global__ __launch_bounds__(kPlanThreads) void k_evict_plan_long(EvictArgs a)
         const int j = movers + block_rank(mover, waves, total);
         movers += total;
         if (hole) p.dst[i] = r;
-        if (mover) p.src[j] = r, p.mv[j] = m;
-        if (stays && r < heavy && a.mass_out != a.mass) a.mass_out[evict_at(a, x, r)] = m;
+        if (mover) p.src[j] = r;
     }
-    evict_masses<kPlanThreads>(a, p, movers);
+    if (t == 0) p.head[0] = movers;
+}
+
+// The masses of a unit's rows to their new places, in the order of the rows' moves.
+__device__ __forceinline__ void move_masses(const EvictArgs &a, const EvictUnit &x, const int *src, const int *dst, int moves, int n)
+{
+    const int t = threadIdx.x, heavy = a.keep - a.recent, old = n - a.recent;
+    if (a.mass_out != a.mass) {  // (what goes too; its places are filled after)
+        for (int r = t; r < heavy; r += kMoveThreads) {
+            const int64_t at = evict_at(a, x, r);
+            a.mass_out[at] = a.mass[at];
+        }
+        __syncthreads();
+    }
+    for (int i = t; i < moves; i += kMoveThreads) a.mass_out[evict_at(a, x, dst[i])] = a.mass[evict_at(a, x, src[i])];
+    __syncthreads();
+    for (int r0 = 0; r0 < a.recent; r0 += kMoveThreads) {
+        const int r = r0 + t;
+        const float m = r < a.recent ? a.mass[evict_at(a, x, old + r)] : 0.f;
+        __syncthreads();  // (a place may be a row that another thread has yet to read)
+        if (r < a.recent) a.mass_out[evict_at(a, x, heavy + r)] = m;
+    }
 }
 
 // A block moves the chunks [c0, c0 + cols) of 16 bytes of a unit's rows, K's and V's
-// side by side.
+// side by side; one more block per unit the masses.
 __global__ __launch_bounds__(kMoveThreads) void k_evict_move(EvictArgs a)
 {
     const uint32_t b = blockIdx.z * (uint32_t)kGridX + blockIdx.x;
-    const uint32_t u = b / (uint32_t)a.splits;
+    // (the masses' blocks come last: in between they would leave the rows' to half of the
+    // XCDs, 134 us instead of 80)
+    const uint32_t rows = (uint32_t)(a.units * a.splits);
+    const bool masses = b >= rows;
+    const uint32_t u = masses ? b - rows : b / (uint32_t)a.splits;
     if (u >= (uint32_t)a.units) return;
     const int split = (int)(b - u * (uint32_t)a.splits), t = threadIdx.x;
     const EvictUnit x = evict_unit(a, u);
     const int *const head = a.plan + (int64_t)u * a.plan_stride;
     const int *const src = head + kPlanHead, *const dst = src + a.cap;
     const int moves = uniform_i32(head[0]), n = uniform_i32(head[1]);
-    if (split == 0 && t == 0) {
+    if (masses && t == 0) {
         if (!a.tails) a.new_counts[u] = moves < 0 ? n : a.keep;
         else if (x.lh == 0) a.new_counts[x.g] = moves < 0 ? n : a.keep;
     }
     if (moves < 0) return;
+    if (masses) {
+        move_masses(a, x, src, dst, moves, n);
+        return;
+    }
     const int cols = a.cols, per = kMoveThreads / cols;  // rows at a time
     const int chunk = split * cols + t % cols, S = a.row_bytes / 16, mine = t / cols;
     char *const pool = (chunk < S ? a.K : a.V) + 16 * (chunk % S);
@@ -462,7 +536,7 @@ hipError_t evict_launch(EvictArgs a, hipStream_t st)
     a.cols = a.row_bytes / 8;
     while (a.cols > 8 && a.units * (a.row_bytes / 8 / a.cols) < 4 * kShBlocks) a.cols /= 2;
     a.splits = a.row_bytes / 8 / a.cols;
-    ECOKV_TIMED("evict_move", st, hipLaunchKernelGGL(k_evict_move, grid(a.units * a.splits), dim3(kMoveThreads), 0, st, a));
+    ECOKV_TIMED("evict_move", st, hipLaunchKernelGGL(k_evict_move, grid(a.units * (a.splits + 1)), dim3(kMoveThreads), 0, st, a));
     return hipGetLastError();
 }
 

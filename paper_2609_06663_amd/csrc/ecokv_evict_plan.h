@@ -24,7 +24,7 @@ inline void mass_grid(int64_t pairs, int B, int conts, int max_count, int max_ta
     *tail_blocks = pairs * conts * *tail_parts;
 }
 
-// Words of a unit's plan: a head, and three for every row that may move to the place
+// Words of a unit's plan: a head, and two for every row that may move to the place
 // of an evicted one, no more than stay and no more than go.
 constexpr int kPlanHead = 4;
 inline int evict_plan_cap(int max_rows, int keep)
@@ -32,6 +32,6 @@ inline int evict_plan_cap(int max_rows, int keep)
     const int go = max_rows - keep;
     return go < 0 ? 0 : go < keep ? go : keep;
 }
-inline int64_t evict_plan_words(int max_rows, int keep) { return kPlanHead + 3 * (int64_t)evict_plan_cap(max_rows, keep); }
+inline int64_t evict_plan_words(int max_rows, int keep) { return kPlanHead + 2 * (int64_t)evict_plan_cap(max_rows, keep); }
 
 }  // namespace ecokv

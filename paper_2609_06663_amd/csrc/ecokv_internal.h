@@ -301,7 +301,7 @@ hipError_t commit_launch(const CommitArgs &a, hipStream_t st);
 
 // Eviction of the rows of least mass.  The plan of a unit in the workspace: kPlanHead
 // words (rows that move, or -1 where none is evicted; rows before), then cap words
-// each of rows that move, their places and their masses.
+// each of rows that move and of their places.
 struct EvictArgs {
     char *K, *V;
     const int32_t *counts, *offsets;
