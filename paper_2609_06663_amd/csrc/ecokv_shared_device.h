@@ -222,6 +222,12 @@ __device__ __forceinline__ void first_tile(const u32x4s *sk, typename ShGeo<BF, 
 template <int NS>
 __device__ __forceinline__ void cut_weights(float y0, float y1, u32x4s (&p)[NS], int j)
 {
+    if constexpr (NS == 1) {  // (one summand: rounded)
+        typedef __bf16 bf16x2s __attribute__((ext_vector_type(2)));
+        typedef float f32x2s __attribute__((ext_vector_type(2)));
+        p[0][j] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2s){y0, y1}, bf16x2s));
+        return;
+    }
 #pragma unroll
     for (int k = 0; k < NS; ++k) {
         p[k][j] = __builtin_amdgcn_perm(__float_as_uint(y1), __float_as_uint(y0), 0x07060302u);

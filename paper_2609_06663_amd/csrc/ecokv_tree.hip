@@ -19,7 +19,7 @@
 
 namespace ecokv {
 
-constexpr int kTreeSummands = 2;  // of a weight in the product with bf16 values
+constexpr int kTreeSummands = 1;  // of a weight in the product with bf16 values
 
 // Drafted rows of a part that need more than the loop does: no page there, or
 // values that are not finite; and whether a tail row has no page.
@@ -115,6 +115,142 @@ __device__ __forceinline__ void add_poison(const TreeArgs &a, const TreeItem &it
     }
 }
 
+// The rows of a part for a block's four tiles of query rows, side by side, two tiles of
+// rows a step: half of the waves load K, half V, one step ahead in registers and the
+// next one in LDS (two places each).  A step is matrix work (logits), vector work
+// (weights), matrix work (values): the two blocks of a compute unit put a wave of each on
+// every SIMD, and one's matrix work runs beside the other's weights.
+//   load(ld, s): the wave's loads of step s;  put(ld, s, ring): into LDS;  mask(t): of
+//   tile t's logits.
+template <bool BF, int D, class Load, class Put, class Mask>
+__device__ __forceinline__ void wide_part(const SharedArgs &a, const SharedItem &it, int q0, int nq, int tiles, Load load, Put put,
+                                          Mask mask, u32x4s *stage, ShState<BF, D, BF ? 32 : 16> &w)
+{
+    constexpr int QT = BF ? 32 : 16;
+    typedef ShGeo<BF, D, QT> Ge;
+    constexpr int NX = Ge::NX;
+    const int lane = threadIdx.x & 63, wq = uniform_i32(threadIdx.x >> 6), grp = lane / QT, row = lane % QT;
+    u32x4s *const ring = wq < kShWaves / 2 ? stage : stage + 4 * Ge::TILE;
+    u32x4s ld[Ge::NL];
+    load(ld, 0);
+    load_queries<BF, D, QT>(a, it, q0, nq, w);
+    put(ld, 0, ring);
+    load(ld, 1);
+    const auto step = [&](int t, int odd) {
+        const u32x4s *const sk = stage + odd * 2 * Ge::TILE, *const sv = sk + 4 * Ge::TILE;
+        // operands are read from LDS AHEAD matrix instructions ahead (the compiler would
+        // read each just before its use, a latency of LDS for every pair)
+        constexpr int AHEAD = 8, NV = 4 * Ge::DT;
+        bf16x8s op[AHEAD];
+        const auto kop = [&](int i) {  // 16 dimensions i / 2 of tile i % 2
+            return __builtin_bit_cast(bf16x8s, sk[i % 2 * Ge::TILE + stage_chunk<BF, Ge::S>(row, 2 * (i / 2) + grp)]);
+        };
+        const auto vop = [&](int i) {  // 16 rows i / DT, tile i % DT of the dimensions
+            const int k = i / Ge::DT, r0 = 16 * (k % 2) + 4 * grp;
+            return value_operand<Ge::S>(sv + k / 2 * Ge::TILE, r0, r0 + 8, 4 * (i % Ge::DT) + 2 * ((lane >> 4) & 1));
+        };
+        lds_barrier();
+        typename Ge::X x[2];
+        if constexpr (BF) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) op[i] = kop(i);
+        }
+        put(ld, t / 2 + 1, ring + (1 - odd) * 2 * Ge::TILE);
+        load(ld, t / 2 + 2);
+        __builtin_amdgcn_sched_barrier(0);
+        if (nq <= 0) return;
+        if constexpr (BF) {
+            x[0] = x[1] = (typename Ge::X){};
+#pragma unroll
+            for (int i = 0; i < 2 * Ge::QS; ++i) {
+                x[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i % AHEAD], __builtin_bit_cast(bf16x8s, w.qb[i / 2]), x[i % 2], 0, 0, 0);
+                op[i % AHEAD] = i + AHEAD < 2 * Ge::QS ? kop(i + AHEAD) : vop(i + AHEAD - 2 * Ge::QS);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+            x[0] = tile_logits<BF, D, QT>(sk, w);
+            x[1] = tile_logits<BF, D, QT>(sk + Ge::TILE, w);
+        }
+        float mb[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            mb[h] = x[h][0];
+#pragma unroll
+            for (int r = 1; r < NX; ++r) mb[h] = fmaxf(mb[h], x[h][r]);
+            mask(t + h)(x[h], mb[h]);
+        }
+        tile_reference<BF, D, QT>(fmaxf(mb[0], mb[1]), a.qscale, w);
+        const float ref = w.m == -INFINITY ? 0.f : w.m;
+        if constexpr (BF) {
+            u32x4s p[2][2][1];  // of tile h, rows 16 k ..
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < NX; e += 2) {
+                    const float y0 = __builtin_amdgcn_exp2f(fmaf(x[h][e], a.qscale, -ref));
+                    const float y1 = __builtin_amdgcn_exp2f(fmaf(x[h][e + 1], a.qscale, -ref));
+                    w.ls += y0 + y1;
+                    cut_weights(y0, y1, p[h][e / 8], e % 8 / 2);
+                }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int k = i / Ge::DT, d = i % Ge::DT;
+                w.acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i % AHEAD], __builtin_bit_cast(bf16x8s, p[k / 2][k % 2][0]), w.acc[d], 0, 0, 0);
+                if (i + AHEAD < NV) op[i % AHEAD] = vop(i + AHEAD);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+            tile_values<BF, D, 3>(sv, x[0], a.qscale, w);
+            tile_values<BF, D, 3>(sv + Ge::TILE, x[1], a.qscale, w);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    for (int t = 0; t < tiles; t += 4) {
+        step(t, 0);
+        if (t + 2 >= tiles) break;
+        step(t + 2, 1);
+    }
+}
+
+// A block's part of a prompt's unit for its four tiles of query rows.
+template <bool BF, int D>
+__device__ __forceinline__ void wide_prompt(const SharedArgs &a, const SharedItem &it, u32x4s *stage)
+{
+    constexpr int QT = BF ? 32 : 16;
+    typedef ShGeo<BF, D, QT> Ge;
+    const int lane = threadIdx.x & 63, wq = uniform_i32(threadIdx.x >> 6);
+    const int q0 = it.q0 + wq * QT, nq = min(it.nq - wq * QT, QT);
+    const bool isk = wq < kShWaves / 2;
+    const int i0 = (wq & 1) * (Ge::NL / 2);  // the wave's load instructions of a tile
+    const int64_t base = (it.base + it.row0) * Ge::RB;
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char *>(uniform_ptr((isk ? a.Kc : a.Vc) + base)), (short)0, uniform_i32((int)((uint32_t)it.rows * Ge::RB)), 0x00020000);
+    // instruction j: of tile 2 s or the next, rows past the part's read zero
+    const auto load = [&](u32x4s (&ld)[Ge::NL], int s) {
+#pragma unroll
+        for (int j = 0; j < Ge::NL; ++j) {
+            const int tile = 2 * s + j / (Ge::NL / 2), i = i0 + j % (Ge::NL / 2);
+            ld[j] = __builtin_bit_cast(u32x4s, __builtin_amdgcn_raw_buffer_load_b128(
+                rs, (int)((uint32_t)(tile * Ge::TR + Ge::RPI * i) * Ge::RB + lane * 16), 0, 0));
+        }
+    };
+    const auto put = [&](const u32x4s (&ld)[Ge::NL], int, u32x4s *ring) {
+#pragma unroll
+        for (int j = 0; j < Ge::NL; ++j) {
+            const int h = j / (Ge::NL / 2), i = i0 + j % (Ge::NL / 2);
+            (ring + h * Ge::TILE)[stage_chunk<BF, Ge::S>(Ge::RPI * i + lane / Ge::S, lane % Ge::S)] = ld[j];
+        }
+    };
+    const auto mask = [&](int t) {
+        const int left = it.rows - t * Ge::TR;
+        return [left](typename Ge::X &x, float &mb) { tile_mask<BF, D, QT>(x, mb, left, 0u); };
+    };
+    ShState<BF, D, QT> w;
+    wide_part<BF, D>(a, it, q0, nq, (it.rows + Ge::TR - 1) / Ge::TR, load, put, mask, stage, w);
+    write_partials<BF, D, QT>(a, it, q0, nq, w);
+}
+
 // A part of a tail and the drafted rows behind it for one tile of query rows, by
 // the four waves of a block (WQ = 4) or by one wave (WQ = 1).
 template <bool BF, int D, int WQ>
@@ -122,7 +258,7 @@ __device__ __forceinline__ void tree_part(const TreeArgs &a, const TreeItem &it,
 {
     constexpr int QT = BF ? 32 : 16, NS = BF ? kTreeSummands : 3;
     typedef ShGeo<BF, D, QT> Ge;
-    constexpr int TR = Ge::TR, LPT = 2 * Ge::NL / WQ;  // load instructions of a wave for a tile
+    constexpr int TR = Ge::TR;
     const int lane = threadIdx.x & 63, wq = WQ == 1 ? 0 : uniform_i32(threadIdx.x >> 6);
     const int seg = lane % Ge::S, rg = lane / Ge::S;
     const int M = a.s.nodes, q0 = it.q0 + wq * QT, nq = min(it.nq - wq * QT, QT);
@@ -196,8 +332,8 @@ __device__ __forceinline__ void tree_part(const TreeArgs &a, const TreeItem &it,
 
     ShState<BF, D, QT> w;
     const int tiles = (it.rows + TR - 1) / TR;
-    typename Ge::X x, y;
     if constexpr (WQ == 1) {
+        typename Ge::X x, y;
         // K a tile ahead of V, as in prompt_part
         u32x4s kx[Ge::NL], vx[Ge::NL];
         unsigned ok = 0, none = 0;
@@ -234,56 +370,34 @@ __device__ __forceinline__ void tree_part(const TreeArgs &a, const TreeItem &it,
             x = y;
         }
     } else {
-        // Half of the waves load K tiles, half V tiles, as in prompt_part: step s puts
-        // K of tile s + 1 and V of tile s.
-        const int isk = wq < WQ / 2, i0 = wq * LPT - (isk ? 0 : Ge::NL);
+        const bool isk = wq < WQ / 2;
+        const int i0 = (wq & 1) * (Ge::NL / 2);
         const char *base = uniform_ptr(isk ? a.s.Kt : a.s.Vt);
         unsigned ok = 0;
-        u32x4s ld[LPT];
-        const auto step = [&](int s, int page) {
+        // pages of a step's two tiles are looked up a step ahead of its loads
+        int next[2] = {pages(0), pages(1)};
+        const auto step = [&](u32x4s (&ld)[Ge::NL], int s) {
 #pragma unroll
-            for (int j = 0; j < LPT; ++j) load(base, i0 + j, s + isk, page, ld[j], ok, j);
-        };
-        const auto put = [&](int s) {
-            u32x4s *const to = stage + (isk ? ((s + 1) & 1) : 2 + (s & 1)) * Ge::TILE;
+            for (int k = 0; k < 2; ++k) {
+                const int pg = next[k];
+                next[k] = pages(2 * s + 2 + k);
 #pragma unroll
-            for (int j = 0; j < LPT; ++j) {
-                if (isk) to[stage_chunk<BF, Ge::S>(Ge::RPI * (i0 + j) + rg, seg)] = ld[j];
-                else put_value(ld[j], ((ok >> j) & 1u) && s >= 0, i0 + j, max(s, 0), to);
+                for (int j = 0; j < Ge::NL / 2; ++j)
+                    load(base, i0 + j, 2 * s + k, pg, ld[k * (Ge::NL / 2) + j], ok, k * (Ge::NL / 2) + j);
+                note(2 * s + k, pg);
             }
         };
-        // (a step's pages are looked up a step ahead of its loads; step -1 of the V waves has none)
-        int pg = pages(max(-1 + isk, 0)), next = pages(isk);
-        step(-1, pg);
-        load_queries<BF, D, QT>(a.s, it, q0, nq, w);
-        lds_barrier();  // (the flags are clear)
-        note(0, pg);
-        put(-1);
-        pg = next, next = pages(1 + isk);
-        note(isk, pg);
-        step(0, pg);
-        put(0);
-        pg = next, next = pages(2 + isk);
-        note(1 + isk, pg);
-        step(1, pg);
-        lds_barrier();
-        first_tile<BF, D, QT>(stage, x, mask(0), a.s.qscale, w);
-        lds_barrier();
-        const auto turn = [&](int t, int odd, typename Ge::X &x, typename Ge::X &y) {
-            put(t + 1);
-            pg = next, next = pages(t + 3 + isk);
-            note(t + 2 + isk, pg);
-            step(t + 2, pg);
-            __builtin_amdgcn_sched_barrier(0);
-            if (nq > 0)
-                tile_step<BF, D, QT, NS>(stage + (1 - odd) * Ge::TILE, stage + (2 + odd) * Ge::TILE, x, y, mask(t + 1), a.s.qscale, w);
-            lds_barrier();
+        const auto put = [&](const u32x4s (&ld)[Ge::NL], int s, u32x4s *ring) {
+#pragma unroll
+            for (int j = 0; j < Ge::NL; ++j) {
+                const int h = j / (Ge::NL / 2), i = i0 + j % (Ge::NL / 2);
+                u32x4s *const to = ring + h * Ge::TILE;
+                if (isk) to[stage_chunk<BF, Ge::S>(Ge::RPI * i + rg, seg)] = ld[j];
+                else put_value(ld[j], (ok >> j) & 1u, i, 2 * s + h, to);
+            }
         };
-        for (int t = 0; t < tiles; t += 2) {
-            turn(t, 0, x, y);
-            if (t + 1 >= tiles) break;
-            turn(t + 1, 1, y, x);
-        }
+        lds_barrier();  // (the flags are clear)
+        wide_part<BF, D>(a.s, it, q0, nq, tiles, step, put, mask, stage, w);
     }
     if constexpr (WQ == 1) wave_lds_order();
     const unsigned long long bad = flags->bad[0] | (unsigned long long)flags->bad[1] << 32;
@@ -310,7 +424,10 @@ __global__ __launch_bounds__(kShThreads, 2) void k_tree(TreeArgs a)
         if (b >= prompts) return;
         SharedItem it;
         prompt_item(a.s, run(b, prompts), it);
-        if (it.rows > 0) prompt_part<BF, D, WQ, BF ? kTreeSummands : 3>(a.s, it, lds);
+        if (it.rows > 0) {
+            if constexpr (WQ == 1) prompt_part<BF, D, 1, BF ? kTreeSummands : 3>(a.s, it, lds);
+            else wide_prompt<BF, D>(a.s, it, lds);
+        }
     } else {
         const uint32_t tb = b - padded, blocks = (uint32_t)a.tails.blocks;
         if (tb >= blocks) return;

@@ -3,9 +3,9 @@ rows, at the sizes, trees, splits, pages and values where they can go wrong.
 
 Tolerance.  dx bounds a logit's error (cache_cases.logit_error).  A weight's relative
 error is at most 2 dx beside its normalisation, weighted sums and merges add fewer
-than 64 roundings; with bf16 rows a weight is cut to 16 bits (two bf16 summands of 8:
-2^-15) and O is rounded to bf16, half a step:
-  |O - O64| <= (2 dx + 2^-18 [+ 2^-15]) max |V| [+ 2^-8 |O64| (1 + 2^-6)],
+than 64 roundings; with bf16 rows a weight w_j is rounded to bf16 in its product with
+the values, half a step of 2^-8 w_j, and O once more at the end:
+  |O - O64| <= (2 dx + 2^-18) max |V| [+ 2^-8 (1 + 2^-6) (sum_j w_j |v_j| + |O64|)],
   |lse - lse64| <= dx + 2^-20 max(1, |lse64|).
 """
 import random
@@ -111,7 +111,7 @@ class Trees(Cache):
                     w = x[live].softmax(-1)
                     ref, rl = w @ V, x[live].logsumexp(-1)
                     dx = logit_error(q.reshape(M * G, D), K, D)
-                    tol = (2 * dx + 2.0 ** -18 + (2.0 ** -15 if bf else 0)) * float(V.abs().max()) + (2.0 ** -8 * (1 + 2.0 ** -6) * ref.abs() if bf else 0)
+                    tol = (2 * dx + 2.0 ** -18) * float(V.abs().max()) + (2.0 ** -8 * (1 + 2.0 ** -6) * (w @ V.abs() + ref.abs()) if bf else 0)
                     err = (got[live] - ref).abs()
                     assert bool((err <= tol).all()), (l, h, c, float((err - tol).max()), dx)
                     assert bool(((gl[live] - rl).abs() <= dx + 2.0 ** -20 * rl.abs().clamp_min(1)).all()), (l, h, c)
