@@ -1311,6 +1311,7 @@ int ecokv_decode_tree(const void *Q_dec, const void *Kc, const void *Vc, int dty
     s.qscale = 1.4426950408889634f / sqrtf((float)si.D);
     s.nodes = num_nodes;
     s.bf16 = bf16;
+    s.tree_rows = a.tails.rows;
     a.masks = reinterpret_cast<const unsigned long long *>(masks);
     a.conts = fan[si.B];
     const hipError_t e = ecokv::tree_launch(a, bf16, static_cast<hipStream_t>(stream));

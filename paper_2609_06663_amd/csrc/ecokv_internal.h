@@ -257,8 +257,8 @@ struct SharedArgs {
     int fan[ECOKV_MAX_SEQS + 1];
     // ecokv_decode_tree: the nodes of a continuation's tree and whether O is bf16.
     // Q, O, N, fan and grid.tile0 are of nodes there, the tails' counts and tables
-    // of continuations.
-    int nodes, bf16;
+    // of continuations; tree_rows: TreeTails::rows.
+    int nodes, bf16, tree_rows;
 };
 hipError_t shared_launch(SharedArgs a, bool bf16, hipStream_t st);
 

@@ -582,7 +582,9 @@ __device__ __forceinline__ ShParts row_parts(const SharedArgs &a, uint32_t qrow)
         const int n = a.tail_counts[TREE ? c / a.nodes : c];
         const bool out = n < 0 || n > a.max_tail;
         r.bad = r.bad || out;
-        r.nt = out ? 0 : parts_used(TREE ? n + a.nodes : n, a.grid.nt, a.grid.tail_step);
+        // (a tree's parts go by the bound)
+        if (TREE) r.nt = out ? 0 : (int)((uint32_t)(n + a.nodes + a.tree_rows - 1) / (uint32_t)a.tree_rows);
+        else r.nt = out ? 0 : parts_used(n, a.grid.nt, a.grid.tail_step);
     }
     return r;
 }

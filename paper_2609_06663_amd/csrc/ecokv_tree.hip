@@ -52,7 +52,9 @@ __device__ __forceinline__ void tree_item(const TreeArgs &a, uint32_t w, TreeIte
     it.h = lh - it.l * a.s.Hkv;
     it.part = g.np + part;
     it.base = 0;
-    item_rows(it, valid ? n + a.s.nodes : 0, a.s.max_tail + a.s.nodes, g.nt, part, g.tail_step);
+    // (parts by the bound, not the count: where a part begins is known before the count is)
+    it.row0 = part * a.tails.rows;
+    it.rows = valid ? uniform_i32(max(min(n + a.s.nodes - it.row0, a.tails.rows), 0)) : 0;
 }
 
 // What lanes of a wave wrote to LDS before is what others read after.
@@ -61,6 +63,19 @@ __device__ __forceinline__ void wave_lds_order()
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
+// x of all lanes, joined.
+__device__ __forceinline__ uint32_t wave_or_u32(uint32_t x)
+{
+    x |= dpp_u32<0xB1>(x);
+    x |= dpp_u32<0x4E>(x);
+    x |= dpp_u32<0x141>(x);
+    x |= dpp_u32<0x140>(x);
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = (uint32_t)r[0] | (uint32_t)r[1];
+    const auto q = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return (uint32_t)q[0] | (uint32_t)q[1];
 }
 
 template <bool BF>
@@ -122,7 +137,8 @@ __device__ __forceinline__ void add_poison(const TreeArgs &a, const TreeItem &it
 // every SIMD, and one's matrix work runs beside the other's weights.
 //   load(ld, s): the wave's loads of step s;  put(ld, s, ring): into LDS;  mask(t): of
 //   tile t's logits.
-template <bool BF, int D, class Load, class Put, class Mask>
+//   TWICE: the code of a step for each of the two places.
+template <bool BF, int D, bool TWICE, class Load, class Put, class Mask>
 __device__ __forceinline__ void wide_part(const SharedArgs &a, const SharedItem &it, int q0, int nq, int tiles, Load load, Put put,
                                           Mask mask, u32x4s *stage, ShState<BF, D, BF ? 32 : 16> &w)
 {
@@ -135,12 +151,12 @@ __device__ __forceinline__ void wide_part(const SharedArgs &a, const SharedItem 
     load(ld, 0);
     load_queries<BF, D, QT>(a, it, q0, nq, w);
     put(ld, 0, ring);
-    load(ld, 1);
+    if (tiles > 2) load(ld, 1);
     const auto step = [&](int t, int odd) {
         const u32x4s *const sk = stage + odd * 2 * Ge::TILE, *const sv = sk + 4 * Ge::TILE;
         // operands are read from LDS AHEAD matrix instructions ahead (the compiler would
         // read each just before its use, a latency of LDS for every pair)
-        constexpr int AHEAD = 8, NV = 4 * Ge::DT;
+        constexpr int AHEAD = TWICE ? 8 : 4, NV = 4 * Ge::DT;
         bf16x8s op[AHEAD];
         const auto kop = [&](int i) {  // 16 dimensions i / 2 of tile i % 2
             return __builtin_bit_cast(bf16x8s, sk[i % 2 * Ge::TILE + stage_chunk<BF, Ge::S>(row, 2 * (i / 2) + grp)]);
@@ -155,8 +171,8 @@ __device__ __forceinline__ void wide_part(const SharedArgs &a, const SharedItem 
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) op[i] = kop(i);
         }
-        put(ld, t / 2 + 1, ring + (1 - odd) * 2 * Ge::TILE);
-        load(ld, t / 2 + 2);
+        if (t + 2 < tiles) put(ld, t / 2 + 1, ring + (1 - odd) * 2 * Ge::TILE);
+        if (t + 4 < tiles) load(ld, t / 2 + 2);
         __builtin_amdgcn_sched_barrier(0);
         if (nq <= 0) return;
         if constexpr (BF) {
@@ -206,10 +222,15 @@ __device__ __forceinline__ void wide_part(const SharedArgs &a, const SharedItem 
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    for (int t = 0; t < tiles; t += 4) {
-        step(t, 0);
-        if (t + 2 >= tiles) break;
-        step(t + 2, 1);
+    if constexpr (TWICE) {
+        for (int t = 0; t < tiles; t += 4) {
+            step(t, 0);
+            if (t + 2 >= tiles) break;
+            step(t + 2, 1);
+        }
+    } else {
+#pragma unroll 1
+        for (int t = 0; t < tiles; t += 2) step(t, (t >> 1) & 1);
     }
 }
 
@@ -247,7 +268,7 @@ __device__ __forceinline__ void wide_prompt(const SharedArgs &a, const SharedIte
         return [left](typename Ge::X &x, float &mb) { tile_mask<BF, D, QT>(x, mb, left, 0u); };
     };
     ShState<BF, D, QT> w;
-    wide_part<BF, D>(a, it, q0, nq, (it.rows + Ge::TR - 1) / Ge::TR, load, put, mask, stage, w);
+    wide_part<BF, D, true>(a, it, q0, nq, (it.rows + Ge::TR - 1) / Ge::TR, load, put, mask, stage, w);
     write_partials<BF, D, QT>(a, it, q0, nq, w);
 }
 
@@ -266,41 +287,62 @@ __device__ __forceinline__ void tree_part(const TreeArgs &a, const TreeItem &it,
     const bool drafted = first < it.rows;
 
     // what this lane's node sees of the drafted rows, and what any node does
+    const unsigned long long within = M < 64 ? (1ull << M) - 1 : ~0ull;
     unsigned long long sees = 0, any = 0;
     if (drafted) {
-        const unsigned long long within = M < 64 ? (1ull << M) - 1 : ~0ull;
         const int m = nq > 0 ? q0 + min(lane % QT, nq - 1) : it.q0;
         sees = a.masks[(int64_t)it.c0 + m % M] & within;
-        any = lane < M ? a.masks[(int64_t)it.c0 + lane] & within : 0;
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) any |= __shfl_xor(any, o, kWave);
+        any = a.masks[(int64_t)it.c0 + min(lane, M - 1)] & within;
     }
     if (WQ == 1 || threadIdx.x == 0) *flags = TreeFlags{};
     if constexpr (WQ == 1) wave_lds_order();
 
-    // the page of this lane's row of a tile (row lane % TR; clamped to the last row), -1 for none
-    const auto pages = [&](int t) { return tail_page(a.s.map, it.c, it.row0 + min(t * TR + lane % TR, it.rows - 1)); };
+    // the page of this lane's row of a tile (row lane % TR; past 2^31 it is negative), -1 for none
+    const auto pages = [&](int t) { return tail_page(a.s.map, it.c, (int)((uint32_t)it.row0 + (uint32_t)(t * TR + lane % TR))); };
     const auto note = [&](int t, int page) {  // rows that have none
-        if (__builtin_amdgcn_ballot_w64(page < 0)) {
+        const unsigned lost = (unsigned)__builtin_amdgcn_ballot_w64(page < 0) & (TR == 32 ? ~0u : (1u << (TR & 31)) - 1u);
+        if (lost) {
             const int r = t * TR + lane;
             if (page < 0 && lane < TR && r < it.rows) {
                 if (r < first) flags->lost = 1;
                 else atomicOr(&flags->bad[(r - first) >> 5], 1u << ((r - first) & 31));
             }
         }
+        return lost;
     };
-    // instruction i of tile t; bit i of ok: the row is there
-    const auto load = [&](const char *base, int i, int t, int page, u32x4s &x, unsigned &ok, int bit) {
-        const int r = t * TR + Ge::RPI * i + rg, pg = __shfl(page, Ge::RPI * i + rg, kWave);
-        const int row = it.row0 + min(r, it.rows - 1);
-        x = *reinterpret_cast<const u32x4s *>(base + tail_row(a.s.map, a.s.Hkv, it.l, it.h, max(pg, 0), row) * Ge::RB + 16 * seg);
-        const bool there = pg >= 0 && r < it.rows && (r < first || ((any >> (r - first)) & 1));
-        ok = there ? ok | (1u << bit) : ok & ~(1u << bit);
+    // The n load instructions from i0 on of tile t (rows without a page: of page 0).  A
+    // page of at least the rows of an instruction has all of them: one address for the
+    // wave, and a lane's place from it never changes.
+    const bool whole = (1 << a.s.map.shift) >= Ge::RPI;
+    const auto load = [&](const char *base, int i0, int t, int page, auto &x, int at, int n) {
+        if (whole) {
+#pragma unroll
+            for (int j = 0; j < n; ++j) {
+                const int pg = __builtin_amdgcn_readlane(page, Ge::RPI * (i0 + j)), row = it.row0 + t * TR + Ge::RPI * (i0 + j);
+                const char *p = uniform_ptr(base + tail_row(a.s.map, a.s.Hkv, it.l, it.h, max(pg, 0), row) * Ge::RB);
+                x[at + j] = *reinterpret_cast<const u32x4s *>(p + (uint32_t)(lane * 16));
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < n; ++j) {
+                const int pg = __shfl(page, Ge::RPI * (i0 + j) + rg, kWave), row = it.row0 + t * TR + Ge::RPI * (i0 + j) + rg;
+                x[at + j] = *reinterpret_cast<const u32x4s *>(
+                    base + tail_row(a.s.map, a.s.Hkv, it.l, it.h, max(pg, 0), row) * Ge::RB + 16 * seg);
+            }
+        }
     };
-    const auto put_value = [&](u32x4s x, bool ok, int i, int t, u32x4s *to) {
-        if (!ok) x = (u32x4s){0u, 0u, 0u, 0u};
-        const int r = t * TR + Ge::RPI * i + rg;
-        if (t * TR + TR > first) {
+    // Staged values (instructions i0 .. i0 + n - 1 of tile t, this wave's own) that are not
+    // to be read as they are: of rows that nobody sees or that have no page (bits of
+    // `lost`), and of drafted rows those that are not finite.  A loop over LDS and not a
+    // part of every store: few tiles need it.
+    const auto mend_values = [&](int i0, int n, int t, unsigned lost, u32x4s *to) {
+        if (t * TR + TR <= min(first, it.rows) && lost == 0) return;
+#pragma unroll 1
+        for (int i = i0; i < i0 + n; ++i) {
+            const int k = Ge::RPI * i + rg, r = t * TR + k;
+            u32x4s *const at = to + stage_chunk<BF, Ge::S>(k, seg);
+            const bool there = !((lost >> k) & 1) && r < it.rows && (r < first || ((any >> (r - first)) & 1));
+            u32x4s x = there ? *at : (u32x4s){0u, 0u, 0u, 0u};
             bool odd = false;
 #pragma unroll
             for (int e = 0; e < 4; ++e) odd = odd || not_finite<BF>(x[e]);
@@ -309,8 +351,11 @@ __device__ __forceinline__ void tree_part(const TreeArgs &a, const TreeItem &it,
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[e] = finite_part<BF>(x[e]);
             }
+            *at = x;
         }
-        to[stage_chunk<BF, Ge::S>(Ge::RPI * i + rg, seg)] = x;
+    };
+    const auto join = [&]() {  // what any node sees
+        if (drafted) any = (unsigned long long)wave_or_u32((uint32_t)(any >> 32)) << 32 | wave_or_u32((uint32_t)any);
     };
     const auto mask = [&](int t) {
         return [&, t](typename Ge::X &x, float &mb) {
@@ -336,18 +381,17 @@ __device__ __forceinline__ void tree_part(const TreeArgs &a, const TreeItem &it,
         typename Ge::X x, y;
         // K a tile ahead of V, as in prompt_part
         u32x4s kx[Ge::NL], vx[Ge::NL];
-        unsigned ok = 0, none = 0;
-        int p0 = pages(0), p1 = pages(1), p2 = pages(2);
+        int p1 = pages(1), p2 = pages(2);
+        unsigned lost;  // of V's tile
         {
             u32x4s k0[Ge::NL];
-#pragma unroll
-            for (int i = 0; i < Ge::NL; ++i) load(a.s.Kt, i, 0, p0, k0[i], none, i);
-#pragma unroll
-            for (int i = 0; i < Ge::NL; ++i) load(a.s.Kt, i, 1, p1, kx[i], none, i);
-#pragma unroll
-            for (int i = 0; i < Ge::NL; ++i) load(a.s.Vt, i, 0, p0, vx[i], ok, i);
+            const int p0 = pages(0);
+            load(a.s.Kt, 0, 0, p0, k0, 0, Ge::NL);
+            load(a.s.Kt, 0, 1, p1, kx, 0, Ge::NL);
+            load(a.s.Vt, 0, 0, p0, vx, 0, Ge::NL);
             load_queries<BF, D, QT>(a.s, it, q0, nq, w);
-            note(0, p0);
+            join();
+            lost = note(0, p0);
 #pragma unroll
             for (int i = 0; i < Ge::NL; ++i) stage[stage_chunk<BF, Ge::S>(Ge::RPI * i + rg, seg)] = k0[i];
         }
@@ -356,13 +400,12 @@ __device__ __forceinline__ void tree_part(const TreeArgs &a, const TreeItem &it,
 #pragma unroll
             for (int i = 0; i < Ge::NL; ++i) {
                 stage[stage_chunk<BF, Ge::S>(Ge::RPI * i + rg, seg)] = kx[i];
-                put_value(vx[i], (ok >> i) & 1u, i, t, stage + Ge::TILE);
+                stage[Ge::TILE + stage_chunk<BF, Ge::S>(Ge::RPI * i + rg, seg)] = vx[i];
             }
-            note(t + 1, p1);
-#pragma unroll
-            for (int i = 0; i < Ge::NL; ++i) load(a.s.Kt, i, t + 2, p2, kx[i], none, i);
-#pragma unroll
-            for (int i = 0; i < Ge::NL; ++i) load(a.s.Vt, i, t + 1, p1, vx[i], ok, i);
+            mend_values(0, Ge::NL, t, lost, stage + Ge::TILE);
+            lost = note(t + 1, p1);
+            load(a.s.Kt, 0, t + 2, p2, kx, 0, Ge::NL);
+            load(a.s.Vt, 0, t + 1, p1, vx, 0, Ge::NL);
             p1 = p2;
             p2 = pages(t + 3);
             __builtin_amdgcn_sched_barrier(0);
@@ -373,31 +416,29 @@ __device__ __forceinline__ void tree_part(const TreeArgs &a, const TreeItem &it,
         const bool isk = wq < WQ / 2;
         const int i0 = (wq & 1) * (Ge::NL / 2);
         const char *base = uniform_ptr(isk ? a.s.Kt : a.s.Vt);
-        unsigned ok = 0;
         // pages of a step's two tiles are looked up a step ahead of its loads
         int next[2] = {pages(0), pages(1)};
+        unsigned lost[2];
         const auto step = [&](u32x4s (&ld)[Ge::NL], int s) {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const int pg = next[k];
                 next[k] = pages(2 * s + 2 + k);
-#pragma unroll
-                for (int j = 0; j < Ge::NL / 2; ++j)
-                    load(base, i0 + j, 2 * s + k, pg, ld[k * (Ge::NL / 2) + j], ok, k * (Ge::NL / 2) + j);
-                note(2 * s + k, pg);
+                load(base, i0, 2 * s + k, pg, ld, k * (Ge::NL / 2), Ge::NL / 2);
+                lost[k] = note(2 * s + k, pg);
             }
         };
         const auto put = [&](const u32x4s (&ld)[Ge::NL], int s, u32x4s *ring) {
 #pragma unroll
-            for (int j = 0; j < Ge::NL; ++j) {
-                const int h = j / (Ge::NL / 2), i = i0 + j % (Ge::NL / 2);
-                u32x4s *const to = ring + h * Ge::TILE;
-                if (isk) to[stage_chunk<BF, Ge::S>(Ge::RPI * i + rg, seg)] = ld[j];
-                else put_value(ld[j], (ok >> j) & 1u, i, 2 * s + h, to);
-            }
+            for (int j = 0; j < Ge::NL; ++j)
+                (ring + j / (Ge::NL / 2) * Ge::TILE)[stage_chunk<BF, Ge::S>(Ge::RPI * (i0 + j % (Ge::NL / 2)) + rg, seg)] = ld[j];
+            if (isk) return;
+            if (s == 0) join();
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) mend_values(i0, Ge::NL / 2, 2 * s + h, h ? lost[1] : lost[0], ring + h * Ge::TILE);
         };
         lds_barrier();  // (the flags are clear)
-        wide_part<BF, D>(a.s, it, q0, nq, tiles, step, put, mask, stage, w);
+        wide_part<BF, D, false>(a.s, it, q0, nq, tiles, step, put, mask, stage, w);
     }
     if constexpr (WQ == 1) wave_lds_order();
     const unsigned long long bad = flags->bad[0] | (unsigned long long)flags->bad[1] << 32;

@@ -10,9 +10,10 @@ namespace ecokv {
 // The tails' part of a call.  A continuation has nodes x G query rows for every
 // (layer, KV head): cut into tiles of wq x rows_q; its tail and the drafted rows
 // behind it into grid.nt parts.  wq = 4: a block takes one tile and one part;
-// wq = 1 (the query rows fit one wave): a wave does.
+// wq = 1 (the query rows fit one wave): a wave does.  Part k has the rows from
+// k * rows on, whatever the count.
 struct TreeTails {
-    int wq, tiles;
+    int wq, tiles, rows;
     int64_t blocks;
 };
 
@@ -61,6 +62,7 @@ inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *f
         g.tail_waves = 0;
         tails->blocks = have * g.nt;
     }
+    tails->rows = (int)part_rows(rows, g.nt, g.tail_step);
     g.bytes = sizeof(float) * (size_t)(g.np + g.nt) * (size_t)g.qrows * (size_t)(D + 2);
     return g;
 }
