@@ -1409,7 +1409,7 @@ int ecokv_accumulate(const void *Q_dec, const float *lse, const void *Kc, int dt
     a.max_count = max_count;
     a.max_tail = max_tail;
     a.decay = decay;
-    const double scale = 1.0 / sqrt((double)si.D);
+    const double scale = 1.4426950408889634074 / sqrt((double)si.D);
     a.scale = (float)scale;
     a.scale_rest = (float)(scale / a.scale - 1.0);
     for (int s = 0; s <= si.B; ++s) a.fan[s] = fan[s];

@@ -17,22 +17,25 @@ typedef unsigned int u32x4e __attribute__((ext_vector_type(4)));
 
 constexpr int kCommitThreads = 256;
 
-// A block moves the K or the V rows of a (layer, KV head, continuation): all of them
-// are in registers before the first is written, so their places may overlap.
+// A wave moves the K or the V rows of a (layer, KV head, continuation), as many at a time
+// as its registers hold, all of these read before the first is written.  Most units have
+// a few rows, so the time is a chain of four loads (accepted, path, page, row): a wave each
+// and not a block lets four times as many run at once (28 layers of 48 continuations, 10
+// rows each on average, us: a block 22.9, a wave 8.5).
 template <int S>
 __global__ __launch_bounds__(kCommitThreads) void k_commit(CommitArgs a)
 {
-    constexpr int EACH = 64 * S / kCommitThreads;  // 16-byte chunks of a thread at most
-    const uint32_t b = blockIdx.z * (uint32_t)kGridX + blockIdx.x;
-    const uint32_t u = b >> 1;
+    const uint32_t w = (blockIdx.z * (uint32_t)kGridX + blockIdx.x) * (kCommitThreads / kWave) + uniform_i32(threadIdx.x >> 6);
+    const uint32_t u = w >> 1;
     if (u >= (uint32_t)a.units) return;
     const int lh = (int)(u / (uint32_t)a.N), c = (int)(u - (uint32_t)lh * (uint32_t)a.N);
     const int l = lh / a.Hkv, h = lh - l * a.Hkv;
     const int lane = threadIdx.x & 63;
     const int n = a.tail_counts[c], take = a.accepted[c];
-    if (n < 0 || take <= 0 || take > a.nodes) return;
     // lane k: from where to where the k-th accepted row goes
-    const int node = lane < take ? a.path[(int64_t)c * a.nodes + lane] : a.nodes + lane;
+    const int path = a.path[(int64_t)c * a.nodes + min(lane, a.nodes - 1)];
+    if (n < 0 || take <= 0 || take > a.nodes) return;
+    const int node = lane < take ? path : a.nodes + lane;
     const int before = __shfl_up(node, 1, kWave);
     const int from = (int)((uint32_t)n + (uint32_t)node), to = (int)((uint32_t)n + (uint32_t)lane);
     int pf = -1, pt = -1;
@@ -41,33 +44,35 @@ __global__ __launch_bounds__(kCommitThreads) void k_commit(CommitArgs a)
         pf = tail_page(a.map, c, from), pt = tail_page(a.map, c, to);
         good = node >= 0 && node < a.nodes && (lane == 0 || node > before) && pf >= 0 && pt >= 0;
     }
-    if (__builtin_amdgcn_ballot_w64(good) != ~0ull) return;  // (the same in every wave)
+    if (__builtin_amdgcn_ballot_w64(good) != ~0ull) return;
     const int stay = __popcll(__builtin_amdgcn_ballot_w64(node == lane));  // (the first ones: the nodes ascend)
-    char *const pool = b & 1 ? a.V : a.K;
+    char *const pool = w & 1 ? a.V : a.K;
     const int chunks = (take - stay) * S;
-    u32x4e x[EACH];
+    constexpr int AT = 8;
+    for (int i0 = 0; i0 < chunks; i0 += AT * kWave) {
+        // (places are below the rows of later turns, which have yet to be read)
+        u32x4e x[AT];
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const int j = i * kCommitThreads + (int)threadIdx.x, k = min(stay + j / S, 63), seg = j % S;
-        if (i * kCommitThreads < chunks) {
+        for (int i = 0; i < AT; ++i) {
+            if (i0 + i * kWave >= chunks) break;
+            const int j = min(i0 + i * kWave + lane, chunks - 1), k = stay + j / S;
             const int r = __shfl(from, k, kWave), page = __shfl(pf, k, kWave);
-            if (j < chunks) x[i] = *reinterpret_cast<const u32x4e *>(pool + tail_row(a.map, a.Hkv, l, h, page, r) * (16 * S) + 16 * seg);
+            x[i] = *reinterpret_cast<const u32x4e *>(pool + tail_row(a.map, a.Hkv, l, h, page, r) * (16 * S) + 16 * (j % S));
         }
-    }
-    __syncthreads();
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (a place may be another's row)
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const int j = i * kCommitThreads + (int)threadIdx.x, k = min(stay + j / S, 63), seg = j % S;
-        if (i * kCommitThreads < chunks) {
+        for (int i = 0; i < AT; ++i) {
+            if (i0 + i * kWave >= chunks) break;
+            const int j = i0 + i * kWave + lane, k = stay + min(j, chunks - 1) / S;
             const int r = __shfl(to, k, kWave), page = __shfl(pt, k, kWave);
-            if (j < chunks) *reinterpret_cast<u32x4e *>(pool + tail_row(a.map, a.Hkv, l, h, page, r) * (16 * S) + 16 * seg) = x[i];
+            if (j < chunks) *reinterpret_cast<u32x4e *>(pool + tail_row(a.map, a.Hkv, l, h, page, r) * (16 * S) + 16 * (j % S)) = x[i];
         }
     }
 }
 
 hipError_t commit_launch(const CommitArgs &a, hipStream_t st)
 {
-    const int64_t n = 2 * a.units;
+    const int64_t n = (2 * a.units + 3) / 4;  // blocks of four waves
     const dim3 g((unsigned)(n < kGridX ? n : kGridX), 1, (unsigned)((n + kGridX - 1) / kGridX)), b(kCommitThreads);
     if (a.row_bytes == 128) ECOKV_TIMED("commit", st, hipLaunchKernelGGL(k_commit<8>, g, b, 0, st, a));
     else if (a.row_bytes == 256) ECOKV_TIMED("commit", st, hipLaunchKernelGGL(k_commit<16>, g, b, 0, st, a));

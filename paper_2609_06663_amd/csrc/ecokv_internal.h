@@ -280,7 +280,7 @@ struct MassArgs {
     float *mass_out, *tail_mass_out;
     int L, Hq, Hkv, G, B, N, D, nodes;
     int max_count, max_tail;
-    float decay, scale, scale_rest;   // 1 / sqrt(D) = scale (1 + scale_rest)
+    float decay, scale, scale_rest;   // log2(e) / sqrt(D) = scale (1 + scale_rest)
     int rt;                           // 16-row tiles of a wave
     int kept_parts, tail_parts;       // blocks of a unit, of a tail
     int64_t kept_blocks, tail_blocks;
