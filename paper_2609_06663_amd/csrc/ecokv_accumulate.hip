@@ -26,7 +26,10 @@ typedef float f32x4m __attribute__((ext_vector_type(4)));
 
 constexpr int kMassThreads = kMassWaves * kWave;
 constexpr int kMassList = 64 * 64;  // nodes that a block lists at a time: 64 continuations of 64
-constexpr int kMassQueries = 16 * kMassWaves;  // query rows that it stages at a time
+// Tiles of 16 query rows staged at a time: six leave room for four blocks on a compute
+// unit and take 96 rows for all of a block's pieces at once (us, accepted paths of four
+// continuations, 28 layers: four tiles 74.6, six 56.4, eight 62.8).
+constexpr int kMassTiles = 6;
 
 template <bool BF, int D>
 struct MassGeo {
@@ -56,15 +59,15 @@ __device__ __forceinline__ f32x4m mass_logits(const u32x4m (&k)[MassGeo<BF, D>::
     }
 }
 
-template <bool BF, int D, int RT>
-__global__ __launch_bounds__(kMassThreads, BF ? 3 : 2) void k_mass(MassArgs a)
+template <bool BF, int D>
+__global__ __launch_bounds__(kMassThreads, BF ? 4 : 3) void k_mass(MassArgs a)
 {
     typedef MassGeo<BF, D> Ge;
-    constexpr int ROWS = 16 * RT;  // of a wave
-    __shared__ int list[kMassList];
-    __shared__ u32x4m qs[kMassWaves][Ge::ST][kWave];  // 16 query rows each, in the order of the operands
-    __shared__ float zs[2][kMassQueries];             // z, and what its roundings leave out
-    __shared__ int lasts[kMassQueries];               // the last row of the tail that a query sees
+    constexpr int RT = kMassRows / 16, ROWS = kMassRows;  // of a wave
+    __shared__ uint16_t list[kMassList];              // nodes, counted from the first listed continuation's; 65535: none
+    __shared__ u32x4m qs[kMassTiles][Ge::ST][kWave];  // 16 query rows each, in the order of the operands
+    __shared__ float zs[2][16 * kMassTiles];          // z, and what its roundings leave out
+    __shared__ int lasts[16 * kMassTiles];            // the last row of the tail that a query sees
     const uint32_t b = blockIdx.z * (uint32_t)kGridX + blockIdx.x;
     const int lane = threadIdx.x & 63, wv = uniform_i32(threadIdx.x >> 6), grp = lane >> 4, row16 = lane & 15;
     const bool tail = b >= (uint32_t)a.kept_blocks;
@@ -118,43 +121,43 @@ __global__ __launch_bounds__(kMassThreads, BF ? 3 : 2) void k_mass(MassArgs a)
             const int xc = __shfl(x, c, kWave), ec = __shfl(end, c, kWave);
             if (k < xc) {
                 const int node = a.path[(int64_t)(cc + c) * a.nodes + k];
-                list[ec - xc + k] = node < 0 || node >= a.nodes ? -1 : (cc + c) * a.nodes + node;
+                list[ec - xc + k] = (uint16_t)(node < 0 || node >= a.nodes ? 65535 : c * a.nodes + node);
             }
         }
         __syncthreads();
         return (int)__builtin_amdgcn_readlane(end, 63);
     };
-    // Query rows qb .. of the listed pairs (continuation, node), a wave 16 of them.
+    // Query rows qb .. of the listed pairs (continuation, node), a wave 16 of them at a time.
     const auto stage = [&](int cc, int queries, int qb) {
         __syncthreads();  // (nobody reads what was staged before)
-        const int q0 = qb + 16 * wv;
-        if (q0 < queries) {
-            const int i = min(q0 + row16, queries - 1);
+        for (int qt = wv; qt < kMassTiles && qb + 16 * qt < queries; qt += kMassWaves) {
+            const int q0 = qb + 16 * qt, i = min(q0 + row16, queries - 1);
             const int p = (int)((uint32_t)i / (uint32_t)a.G), g = i - p * a.G;
-            const int node = a.path ? list[p] : cc + p;
-            const int64_t qrow = ((int64_t)l * a.Hq + h * a.G + g) * ((int64_t)a.N * a.nodes) + max(node, 0);
+            const int entry = a.path ? list[p] : p;
+            const bool none = entry == 65535 && a.path;
+            const int64_t qrow = ((int64_t)l * a.Hq + h * a.G + g) * ((int64_t)a.N * a.nodes) + (int64_t)cc * a.nodes + (none ? 0 : entry);
             const char *qp = a.Q + qrow * Ge::RB + 16 * grp;
             u32x4m q[Ge::ST];
 #pragma unroll
             for (int s = 0; s < Ge::ST; ++s) q[s] = *reinterpret_cast<const u32x4m *>(qp + 64 * s);
             float lse = a.lse[qrow];
 #pragma unroll
-            for (int s = 0; s < Ge::ST; ++s) qs[wv][s][lane] = q[s];
+            for (int s = 0; s < Ge::ST; ++s) qs[qt][s][lane] = q[s];
             // a query that is not there, or that saw no row, weighs nothing
-            if (node < 0 || q0 + row16 >= queries || lse == -INFINITY) lse = INFINITY;
+            if (none || q0 + row16 >= queries || lse == -INFINITY) lse = INFINITY;
             constexpr float kLog2e = 1.44269504f, kLog2eRest = 1.92596299e-8f;
             const float z = lse * kLog2e;
             if (grp == 0) {
-                zs[0][16 * wv + row16] = z;
-                zs[1][16 * wv + row16] = fabsf(z) < INFINITY ? z * a.scale_rest - fmaf(lse, kLog2eRest, fmaf(lse, kLog2e, -z)) : 0.f;
-                lasts[16 * wv + row16] = tail ? n - fresh + p : 0;
+                zs[0][16 * qt + row16] = z;
+                zs[1][16 * qt + row16] = fabsf(z) < INFINITY ? z * a.scale_rest - fmaf(lse, kLog2eRest, fmaf(lse, kLog2e, -z)) : 0.f;
+                lasts[16 * qt + row16] = tail ? n - fresh + p : 0;
             }
         }
         __syncthreads();
     };
     // where they fit, one list and one stage serve all of the block's rows
     const int all = c1 - c0 > 64 ? INT32_MAX : (a.path ? enlist(c0, c1 - c0) : c1 - c0) * a.G;
-    const bool once = all <= kMassQueries;
+    const bool once = all <= 16 * kMassTiles;
     if (once && all > 0) stage(c0, all, 0);
 
     for (int64_t first = (int64_t)part * BLOCK; first < n; first += stride) {
@@ -188,9 +191,9 @@ __global__ __launch_bounds__(kMassThreads, BF ? 3 : 2) void k_mass(MassArgs a)
         for (int cc = c0; cc < c1; cc += 64) {
             const int nc = min(c1 - cc, 64);
             const int queries = once || all != INT32_MAX ? all : (a.path ? enlist(cc, nc) : nc) * a.G;
-            for (int qb = 0; qb < queries; qb += kMassQueries) {
+            for (int qb = 0; qb < queries; qb += 16 * kMassTiles) {
                 if (!once) stage(cc, queries, qb);
-                for (int qt = 0; qt < kMassWaves && qb + 16 * qt < queries; ++qt) {
+                for (int qt = 0; qt < kMassTiles && qb + 16 * qt < queries; ++qt) {
                     u32x4m q[Ge::ST];
 #pragma unroll
                     for (int s = 0; s < Ge::ST; ++s) q[s] = qs[qt][s][lane];
@@ -225,22 +228,15 @@ __global__ __launch_bounds__(kMassThreads, BF ? 3 : 2) void k_mass(MassArgs a)
     }
 }
 
-template <bool BF, int D>
-static void launch_mass(const MassArgs &a, dim3 grid, hipStream_t st)
-{
-    if (a.rt == 4) hipLaunchKernelGGL((k_mass<BF, D, 4>), grid, dim3(kMassThreads), 0, st, a);
-    else hipLaunchKernelGGL((k_mass<BF, D, 2>), grid, dim3(kMassThreads), 0, st, a);
-}
-
 hipError_t mass_launch(const MassArgs &a, bool bf16, hipStream_t st)
 {
     const int64_t n = a.kept_blocks + a.tail_blocks;
     if (n == 0) return hipSuccess;
     const dim3 g((unsigned)(n < kGridX ? n : kGridX), 1, (unsigned)((n + kGridX - 1) / kGridX));
-    if (bf16 && a.D == 128) ECOKV_TIMED("accumulate", st, (launch_mass<true, 128>(a, g, st)));
-    else if (bf16) ECOKV_TIMED("accumulate", st, (launch_mass<true, 64>(a, g, st)));
-    else if (a.D == 128) ECOKV_TIMED("accumulate", st, (launch_mass<false, 128>(a, g, st)));
-    else ECOKV_TIMED("accumulate", st, (launch_mass<false, 64>(a, g, st)));
+    if (bf16 && a.D == 128) ECOKV_TIMED("accumulate", st, hipLaunchKernelGGL((k_mass<true, 128>), g, dim3(kMassThreads), 0, st, a));
+    else if (bf16) ECOKV_TIMED("accumulate", st, hipLaunchKernelGGL((k_mass<true, 64>), g, dim3(kMassThreads), 0, st, a));
+    else if (a.D == 128) ECOKV_TIMED("accumulate", st, hipLaunchKernelGGL((k_mass<false, 128>), g, dim3(kMassThreads), 0, st, a));
+    else ECOKV_TIMED("accumulate", st, hipLaunchKernelGGL((k_mass<false, 64>), g, dim3(kMassThreads), 0, st, a));
     return hipGetLastError();
 }
 

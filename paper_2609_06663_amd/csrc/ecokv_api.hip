@@ -1413,7 +1413,7 @@ int ecokv_accumulate(const void *Q_dec, const float *lse, const void *Kc, int dt
     a.scale = (float)scale;
     a.scale_rest = (float)(scale / a.scale - 1.0);
     for (int s = 0; s <= si.B; ++s) a.fan[s] = fan[s];
-    ecokv::mass_grid((int64_t)si.L * si.Hkv, si.B, tailed ? N : 0, max_count, max_tail, &a.rt, &a.kept_parts, &a.tail_parts,
+    ecokv::mass_grid((int64_t)si.L * si.Hkv, si.B, tailed ? N : 0, max_count, max_tail, &a.kept_parts, &a.tail_parts,
                      &a.kept_blocks, &a.tail_blocks);
     if (a.kept_blocks > INT32_MAX - (1 << 20) || a.tail_blocks > INT32_MAX - (1 << 20) - a.kept_blocks)
         return fail(ECOKV_EINVAL, "too many parts of kept rows or tails");

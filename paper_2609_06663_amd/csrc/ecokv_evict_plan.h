@@ -7,22 +7,23 @@
 
 namespace ecokv {
 
-constexpr int kMassWaves = 4;  // waves per block
+constexpr int kMassWaves = 4;   // waves per block
+constexpr int kMassRows = 32;   // rows of a wave at a time
 
-// Blocks of ecokv_accumulate: a wave takes rt tiles of 16 rows of a unit or a tail at a
-// time, a block four waves.  Where there are more than kMassBlocks such pieces, a block
-// takes several of its unit's, `parts` apart: the queries are listed once for all of them
-// (accepted paths of four continuations, 28 layers of 6553 kept rows, us: a piece a block
-// 100, three 78).
+// Blocks of ecokv_accumulate: a block takes four waves' rows of a unit or a tail at a
+// time.  Where there are more than kMassBlocks such pieces, it takes several of its
+// unit's, `parts` apart: the queries are listed and staged once for all of them.  (Us,
+// 28 layers of 6553 kept rows and four tails of 777, one query of each and accepted
+// paths: a piece a block 59.7 and 85.0, 3072 blocks 50.1 and 76.7, 1536 blocks 49.0 and
+// 75.0, 768 blocks 55.3 and 82.7; 64 rows of a wave and 1536 blocks 55.4 and 78.6.)
 constexpr int kMassBlocks = 1536;
-inline void mass_grid(int64_t pairs, int B, int conts, int max_count, int max_tail, int *rt, int *kept_parts, int *tail_parts,
+inline void mass_grid(int64_t pairs, int B, int conts, int max_count, int max_tail, int *kept_parts, int *tail_parts,
                       int64_t *kept_blocks, int64_t *tail_blocks)
 {
     const auto pieces = [](int64_t rows, int64_t each) { return (rows + each - 1) / each; };
-    const auto all = [&](int64_t each) { return pairs * B * pieces(max_count, each) + pairs * conts * pieces(max_tail, each); };
-    *rt = all(64 * kMassWaves) >= 1024 ? 4 : 2;
-    const int each = 16 * *rt * kMassWaves;
-    const int64_t several = (all(each) + kMassBlocks - 1) / kMassBlocks, s = several < 1 ? 1 : several > 8 ? 8 : several;
+    const int64_t each = kMassRows * kMassWaves;
+    const int64_t all = pairs * B * pieces(max_count, each) + pairs * conts * pieces(max_tail, each);
+    const int64_t several = (all + kMassBlocks - 1) / kMassBlocks, s = several < 1 ? 1 : several > 8 ? 8 : several;
     *kept_parts = (int)pieces(max_count, each * s);
     *tail_parts = conts > 0 ? (int)pieces(max_tail, each * s) : 0;
     *kept_blocks = pairs * B * *kept_parts;

@@ -281,7 +281,6 @@ struct MassArgs {
     int L, Hq, Hkv, G, B, N, D, nodes;
     int max_count, max_tail;
     float decay, scale, scale_rest;   // log2(e) / sqrt(D) = scale (1 + scale_rest)
-    int rt;                           // 16-row tiles of a wave
     int kept_parts, tail_parts;       // blocks of a unit, of a tail
     int64_t kept_blocks, tail_blocks;
     TailMap map;
