@@ -17,16 +17,17 @@ typedef unsigned int u32x4e __attribute__((ext_vector_type(4)));
 
 constexpr int kCommitThreads = 256;
 
-// A wave moves the K or the V rows of a (layer, KV head, continuation), as many at a time
-// as its registers hold, all of these read before the first is written.  Most units have
-// a few rows, so the time is a chain of four loads (accepted, path, page, row): a wave each
-// and not a block lets four times as many run at once (28 layers of 48 continuations, 10
-// rows each on average, us: a block 22.9, a wave 8.5).
+// A wave moves the rows of a (layer, KV head, continuation), as many at a time as its
+// registers hold, all of these read before the first is written.  Most units have a few
+// rows, so the time is a chain of four loads (accepted, path, page, row): a wave each and
+// not a block lets more run at once (28 layers of 48 continuations, 15 rows each on
+// average, us: a block for K and one for V 22.9, a wave each 17.0, a wave for both 16.5,
+// 82 MB at 5.0 TB/s).
 template <int S>
 __global__ __launch_bounds__(kCommitThreads) void k_commit(CommitArgs a)
 {
     const uint32_t w = (blockIdx.z * (uint32_t)kGridX + blockIdx.x) * (kCommitThreads / kWave) + uniform_i32(threadIdx.x >> 6);
-    const uint32_t u = w >> 1;
+    const uint32_t u = w;
     if (u >= (uint32_t)a.units) return;
     const int lh = (int)(u / (uint32_t)a.N), c = (int)(u - (uint32_t)lh * (uint32_t)a.N);
     const int l = lh / a.Hkv, h = lh - l * a.Hkv;
@@ -46,18 +47,19 @@ __global__ __launch_bounds__(kCommitThreads) void k_commit(CommitArgs a)
     }
     if (__builtin_amdgcn_ballot_w64(good) != ~0ull) return;
     const int stay = __popcll(__builtin_amdgcn_ballot_w64(node == lane));  // (the first ones: the nodes ascend)
-    char *const pool = w & 1 ? a.V : a.K;
     const int chunks = (take - stay) * S;
-    constexpr int AT = 8;
+    constexpr int AT = 8;  // loads of each in a row
     for (int i0 = 0; i0 < chunks; i0 += AT * kWave) {
         // (places are below the rows of later turns, which have yet to be read)
-        u32x4e x[AT];
+        u32x4e x[2][AT];
 #pragma unroll
         for (int i = 0; i < AT; ++i) {
             if (i0 + i * kWave >= chunks) break;
             const int j = min(i0 + i * kWave + lane, chunks - 1), k = stay + j / S;
             const int r = __shfl(from, k, kWave), page = __shfl(pf, k, kWave);
-            x[i] = *reinterpret_cast<const u32x4e *>(pool + tail_row(a.map, a.Hkv, l, h, page, r) * (16 * S) + 16 * (j % S));
+            const int64_t at = tail_row(a.map, a.Hkv, l, h, page, r) * (16 * S) + 16 * (j % S);
+            x[0][i] = *reinterpret_cast<const u32x4e *>(a.K + at);
+            x[1][i] = *reinterpret_cast<const u32x4e *>(a.V + at);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (a place may be another's row)
 #pragma unroll
@@ -65,14 +67,18 @@ __global__ __launch_bounds__(kCommitThreads) void k_commit(CommitArgs a)
             if (i0 + i * kWave >= chunks) break;
             const int j = i0 + i * kWave + lane, k = stay + min(j, chunks - 1) / S;
             const int r = __shfl(to, k, kWave), page = __shfl(pt, k, kWave);
-            if (j < chunks) *reinterpret_cast<u32x4e *>(pool + tail_row(a.map, a.Hkv, l, h, page, r) * (16 * S) + 16 * (j % S)) = x[i];
+            const int64_t at = tail_row(a.map, a.Hkv, l, h, page, r) * (16 * S) + 16 * (j % S);
+            if (j < chunks) {
+                *reinterpret_cast<u32x4e *>(a.K + at) = x[0][i];
+                *reinterpret_cast<u32x4e *>(a.V + at) = x[1][i];
+            }
         }
     }
 }
 
 hipError_t commit_launch(const CommitArgs &a, hipStream_t st)
 {
-    const int64_t n = (2 * a.units + 3) / 4;  // blocks of four waves
+    const int64_t n = (a.units + 3) / 4;  // blocks of four waves
     const dim3 g((unsigned)(n < kGridX ? n : kGridX), 1, (unsigned)((n + kGridX - 1) / kGridX)), b(kCommitThreads);
     if (a.row_bytes == 128) ECOKV_TIMED("commit", st, hipLaunchKernelGGL(k_commit<8>, g, b, 0, st, a));
     else if (a.row_bytes == 256) ECOKV_TIMED("commit", st, hipLaunchKernelGGL(k_commit<16>, g, b, 0, st, a));

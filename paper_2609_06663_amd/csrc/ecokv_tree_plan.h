@@ -17,6 +17,8 @@ struct TreeTails {
     int64_t blocks;
 };
 
+constexpr int kTreeRows = 512;  // rows of a prompt's part that are worth a block of its own
+
 // fan counts nodes (fan[s + 1] - fan[s] of prompt s); conts continuations.
 inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *fan, int conts, int nodes, int max_count,
                             int max_tail, bool bf16, TreeTails *tails)
@@ -38,27 +40,44 @@ inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *f
     for (int s = 0; s < B; ++s) g.tile0[s + 1] = g.tile0[s] + (int)(((int64_t)G * (fan[s + 1] - fan[s]) + qt - 1) / qt);
     g.tiles = max_count > 0 ? g.tile0[B] : 0;
     g.qrows = pairs * G * fan[B];
-    g.np = prompt_parts(g, pairs * g.tiles, pairs * prompts, D, max_count, bf16);
-    g.prompt_blocks = pairs * g.tiles * g.np;
-
     const int rows = max_tail + nodes;
     tails->wq = nodes * G <= g.rows_q ? 1 : 4;
     const int tt = tails->wq * g.rows_q;
     tails->tiles = (nodes * G + tt - 1) / tt;
-    const int64_t have = pairs * conts * tails->tiles;
+    const int64_t have = pairs * conts * tails->tiles;  // (continuation, tile)s
+    const int64_t slots = 2 * kShBlocks;                // blocks that run at once
+    const int64_t prompt_have = pairs * g.tiles, tail_least = tails->wq == 1 ? (have + kShWaves - 1) / kShWaves : have;
+
+    g.np = prompt_parts(g, prompt_have, pairs * prompts, D, max_count, bf16);
+    if (g.wq == 4 && g.np > 0) {
+        // two blocks per compute unit where the parts stay long
+        const int64_t fill = (slots - tail_least) / prompt_have, most = max_count / kTreeRows;
+        const int64_t np = fill < most ? fill : most;
+        if (np > g.np) g.np = parts_within(np, max_count, g.step);
+    }
+    g.prompt_blocks = prompt_have * g.np;
+
     if (tails->wq == 1) {
+        // waves: one for each SIMD, or two while their parts stay long
         g.tail_step = 2 * g.rows_t;
-        g.nt = tail_parts(g.np == 0, have, rows, g.tail_step);
+        const int64_t one = kShBlocks * kShWaves / have, two = 2 * kShBlocks * kShWaves / have;
+        g.nt = parts_within(two > one && rows / two >= 256 ? two : one < 1 ? 1 : one, rows, g.tail_step);
         g.tail_waves = have * g.nt;
         tails->blocks = (g.tail_waves + kShWaves - 1) / kShWaves;
     } else {
-        g.tail_step = g.rows_t;
+        // as many as there is room for beside the prompts, none short, and none longer
+        // than a prompt's part
+        g.tail_step = 2 * g.rows_t;
+        int64_t nt;
         if (g.np > 0) {
-            const int64_t like = ((int64_t)max_count + g.np - 1) / g.np;  // rows of a prompt's part
-            g.nt = parts_within((rows + like - 1) / like, rows, g.tail_step);
+            const int64_t like = ((int64_t)max_count + g.np - 1) / g.np, least = (rows + like - 1) / like;
+            const int64_t room = (slots - g.prompt_blocks) / have, most = rows / (4 * g.rows_t);
+            nt = room < most ? room : most;
+            nt = nt > least ? nt : least;
         } else {
-            g.nt = prompt_parts(g, have, pairs * conts, D, rows, bf16);
+            nt = prompt_parts(g, have, pairs * conts, D, rows, bf16);
         }
+        g.nt = parts_within(nt < 1 ? 1 : nt, rows, g.tail_step);
         g.tail_waves = 0;
         tails->blocks = have * g.nt;
     }

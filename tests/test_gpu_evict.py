@@ -258,6 +258,10 @@ TAILS = [  # dtype, L, Hkv, D, page, limit, keep, recent, tails, masses
     ("bf16", 1, 1, 128, 256, 9000, 9000, 77, [20000, 9001], "ties"),
     ("f32", 1, 2, 128, 16, 2500, 2500, 2000, [2600, 4999, 2501], "old"),
     ("bf16", 2, 1, 64, 64, 700, 350, 349, [701, 1400], "old"),
+    # many units
+    ("bf16", 28, 4, 64, 16, 200, 150, 40, [201, 300, 150, 90, 777], "ties"),
+    ("f32", 32, 4, 128, 8, 300, 300, 290, [310, 301, 1, 590], "odd"),
+    ("bf16", 16, 32, 64, 64, 20, 10, 0, [21, 2048], "same"),
 ]
 
 
@@ -298,6 +302,8 @@ KEPT = [  # dtype, L, Hkv, D, limit, keep, recent, counts (per prompt), masses
     ("f32", 1, 2, 64, 2000, 2000, 0, [6553, 2001], "ties"),
     ("bf16", 1, 1, 128, 17, 16, 16, [6000, 18], "odd"),
     ("bf16", 4, 8, 128, 2047, 2047, 8, [2800, 4000], "old"),
+    ("bf16", 32, 8, 64, 100, 80, 70, [300, 120, 90], "ties"),
+    ("f32", 32, 8, 64, 1000, 1000, 1, [1300, 1001], "odd"),
 ]
 
 
