@@ -564,9 +564,10 @@ int ecokv_decode_tree_workspace_size(const ecokv_shape *shape, const int32_t *fa
  * rows unwritten.  A tail row without a page in [0, num_pages) gives NaN outputs for
  * its continuation, a drafted row without one for the nodes that see it, a count out
  * of its bounds for the continuations concerned.
- * Arithmetic: fp32 accumulation (bf16 rows: the weights as two bf16 summands each, 16
- * bits, beside an output of 8; among kept rows and the tail's a value row with an
- * infinity gives NaN).
+ * Arithmetic: logits, maxima, sums and accumulation in fp32.  With bf16 rows a weight
+ * is rounded to bf16 where it multiplies a value (its own sum takes it unrounded), half
+ * a step of 2^-8, as O is rounded to bf16 itself.  An infinity among the values of kept
+ * rows or the tail's may give NaN in its dimension.
  * Alignment, workspace and repeatability as ecokv_decode_shared; outputs and the
  * workspace overlap neither Q_dec nor the tails nor each other. */
 int ecokv_decode_tree(const void *Q_dec, const void *Kc, const void *Vc, int dtype, const ecokv_shape *shape,
@@ -628,7 +629,8 @@ int ecokv_accumulate(const void *Q_dec, const float *lse, const void *Kc, int dt
 
 /* Workspace bytes of ecokv_evict (groups: the shape's sequences) and
  * ecokv_evict_tails (groups: the continuations) for a bound of max_rows rows of which
- * `keep` stay.  Larger keeps may need less. */
+ * `keep` stay: 16 bytes of a unit and 8 for each of min(keep, max_rows - keep) rows,
+ * the most that can move. */
 int ecokv_evict_workspace_size(const ecokv_shape *shape, int32_t groups, int32_t max_rows, int32_t keep, size_t *bytes);
 
 /* Eviction from the compressed cache.  A unit u with n = counts[u] > limit rows keeps

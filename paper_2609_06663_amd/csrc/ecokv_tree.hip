@@ -19,7 +19,12 @@
 
 namespace ecokv {
 
-constexpr int kTreeSummands = 1;  // of a weight in the product with bf16 values
+// bf16 summands of a weight in its product with bf16 values: one, rounded.  Its half
+// step of 2^-8 stands beside O's own; the weights' sum takes them unrounded.  (28
+// layers of 4 KV heads with 6553 rows, 8 continuations of 130 rows and 16 nodes, with
+// one, two and three: 469, 577 and 712 us; largest error against 64 bits, of values
+// around 1: 0.0023 with one, 0.0017 of a form whose O alone is rounded.)
+constexpr int kTreeSummands = 1;
 
 // Drafted rows of a part that need more than the loop does: no page there, or
 // values that are not finite; and whether a tail row has no page.

@@ -875,6 +875,8 @@ def ecokv_commit(shape: Shape, tails: Tails, tail_counts: torch.Tensor, path: to
     c = shape.c
     if c.num_layers == 0:
         return
+    if tails is None:
+        raise ValueError("tails is required")
     dev, dt, code = _first(tails.K, "the tails' K")
     N = tails.table.shape[0]
     M = _per_node(path, "path", torch.int32, N, dev)
@@ -969,6 +971,8 @@ def ecokv_evict_tails(shape: Shape, tails: Tails, tail_counts: torch.Tensor, max
     c = shape.c
     if c.num_layers == 0:
         return
+    if tails is None:
+        raise ValueError("tails is required")
     dev, dt, code = _first(tails.K, "the tails' K")
     N = tails.table.shape[0]
     if N == 0:
