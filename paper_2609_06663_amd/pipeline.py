@@ -154,8 +154,8 @@ class LayerwiseEviction:
 class Continuations:
     """Generation from the compressed prompts of an `EvictionPass`.
 
-    Prompt s is continued by fan_out[s] continuations of up to `max_new` tokens
-    each, whose keys and values lie in paged tails; all continuations of a
+    Prompt s is continued by fan_out[s] continuations whose tails hold up to
+    `max_new` tokens each, keys and values in pages; all continuations of a
     prompt share its kept rows.  For every generated token, `step` takes the new
     queries, keys and values as the projections wrote them ([L][N][heads][D],
     views of a fused tensor will do), norms and rotates queries and keys (`rope`),
@@ -167,15 +167,25 @@ class Continuations:
     with a pass per layer, each layer has its own instance, advanced with the
     others.
 
-    `step` and `advance` only enqueue work, on one stream at a time (they share a
+    With `max_nodes` > 0 several drafted tokens of each continuation are attended
+    at once: `tree` lays out what sees what, `draft` takes the place of `step` and
+    `commit` of `advance`, which adds to each tail the nodes that were accepted,
+    as many as there are.  With `masses`, `accumulate` after a step or a commit
+    adds up what weight every row gets (`mass`, `tail_mass`), and between tokens
+    `evict` bounds the tails and `evict_kept` the prompts' rows (of the pass
+    itself) by dropping those of the least: with a limit below `max_new`
+    generation need not end.
+
+    The calls only enqueue work, on one stream at a time (they share a
     workspace): `advance` goes where the last `step` went, to the stream that it
     was given or else to the current one.  Who changes the stream between calls
-    orders the one after the other.  To capture them in a HIP graph, pass `step`
-    max_tail=max_new: by default it is the present length, which a replay would
-    not raise.  A replay moves the device's counters only; `length` is the
-    caller's to keep."""
+    orders the one after the other.  To capture them in a HIP graph, pass them
+    max_tail (max_new, or the limit's bound): by default it is the present length,
+    which a replay would not raise.  A replay moves the device's counters only;
+    `length`, the tails' rows or more, is the caller's to keep."""
 
-    def __init__(self, ep: EvictionPass, fan_out, max_new: int, rope: E.Rope, page_size: int = 64):
+    def __init__(self, ep: EvictionPass, fan_out, max_new: int, rope: E.Rope, page_size: int = 64, max_nodes: int = 0,
+                 masses: bool = False):
         shape = ep.shape
         c = shape.c
         fan_out = E._flat_ints(fan_out)
@@ -185,14 +195,18 @@ class Continuations:
             raise ValueError("fan_out has no continuation")
         if max_new < 1:
             raise ValueError(f"max_new {max_new} < 1")
-        self.ep, self.rope, self.max_new, self.length = ep, rope, int(max_new), 0
+        if not 0 <= max_nodes <= E.MAX_NODES:
+            raise ValueError(f"max_nodes {max_nodes} outside [0, {E.MAX_NODES}]")
+        self.ep, self.rope, self.max_new, self.max_nodes, self.length = ep, rope, int(max_new), int(max_nodes), 0
         self._stream = None  # that the last step was given
+        self._pending = None  # "step" or "draft": rows that are not the tails' yet
+        self._unweighed = None  # "step", or the path of a commit: what accumulate may add
         self.fan = [0]
         for f in fan_out:
             self.fan.append(self.fan[-1] + f)
         N, L, Hq, Hkv, D = self.fan[-1], c.num_layers, c.num_q_heads, c.num_kv_heads, c.head_dim
         dev, dtype = ep.Kc.device, ep.Kc.dtype
-        per = -(-self.max_new // page_size)
+        per = -(-(self.max_new + self.max_nodes) // page_size)
         self.tails = E.Tails(*(torch.empty((L, N * per, Hkv, page_size, D), dtype=dtype, device=dev) for _ in range(2)),
                              torch.arange(N * per, dtype=torch.int32, device=dev).view(N, per))
         cu = shape.cu_seqlens
@@ -211,8 +225,26 @@ class Continuations:
         self.Q_dec = torch.empty((L, Hq, N, D), dtype=dtype, device=dev)
         self.O = torch.empty((L, Hq, N, D), dtype=torch.float32, device=dev)
         self.lse = torch.empty((L, Hq, N), dtype=torch.float32, device=dev)
-        self.workspace = torch.empty(
-            max(E.ecokv_decode_shared_workspace_size(shape, self.fan, self.max_count, self.max_new), 256), dtype=torch.uint8, device=dev)
+        need = max(E.ecokv_decode_shared_workspace_size(shape, self.fan, self.max_count, self.max_new), 256)
+        if self.max_nodes:
+            need = max(need, E.ecokv_decode_tree_workspace_size(shape, self.fan, self.max_count, self.max_new, self.max_nodes))
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        self._outgrown = []  # workspaces that a captured graph may still use
+        # of drafts: of max_nodes nodes each, of fewer the beginning
+        n = L * Hq * N * self.max_nodes
+        self._nodes = torch.empty(n * D, dtype=dtype, device=dev), torch.empty(n * D, dtype=dtype, device=dev), torch.empty(n, device=dev)
+        self.Q_nodes = self.O_nodes = self.lse_nodes = None
+        self.mass = self.tail_mass = None
+        if masses:
+            self.mass = torch.zeros(ep.Kc.shape[0], dtype=torch.float32, device=dev)
+            self.tail_mass = torch.zeros((L, N * per, Hkv, page_size), dtype=torch.float32, device=dev)
+
+    def _need(self, nbytes: int, stream) -> None:
+        """A workspace of nbytes (in order with `stream`, where it is given)."""
+        if self.workspace.numel() < nbytes:
+            self._outgrown.append(self.workspace)
+            with torch.cuda.stream(stream):  # (None: the current stream stays)
+                self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.workspace.device)
 
     def step(self, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, stream=None, max_tail: Optional[int] = None) -> torch.Tensor:
         """Append the next token of every continuation and attend; returns O."""
@@ -226,10 +258,136 @@ class Continuations:
         E.ecokv_decode_shared(self.Q_dec, self.ep.Kc, self.ep.Vc, self.ep.shape, self.fan, self.ep.counts, self.ep.offsets, self.max_count,
                               self.tails, self.tail_counts, self.length + 1 if max_tail is None else max_tail, self.O, self.lse,
                               self.workspace, stream)
+        self._pending = self._unweighed = "step"
         return self.O
 
     def advance(self, stream=None) -> None:
         """On to the next token (enqueued on `stream`, or else on the last step's)."""
+        if self._pending == "draft":
+            raise ValueError("a draft goes on with commit")
         with torch.cuda.stream(self._stream if stream is None else stream):  # (None: the current stream stays)
             self._at.add_(1)
+        self._pending = None
         self.length += 1
+
+    def tree(self, parents) -> "Tree":
+        """Trees for `draft`: the parents of each node (earlier nodes, or -1: the tail's
+        last token), one list for all continuations or one for each, of up to max_nodes
+        nodes; where they differ in length, the shorter ones are padded."""
+        N = self.fan[-1]
+        lists = [list(p) for p in parents] if len(parents) and not isinstance(parents[0], int) else [list(parents)] * N
+        if len(lists) != N:
+            raise ValueError(f"{len(lists)} trees for {N} continuations")
+        M = max(map(len, lists))
+        if not 1 <= M <= self.max_nodes:
+            raise ValueError(f"a tree of {M} nodes, max_nodes is {self.max_nodes}")
+        return Tree(lists, M, self.rows.device)
+
+    def draft(self, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, tree: "Tree", stream=None,
+              max_tail: Optional[int] = None) -> torch.Tensor:
+        """Append the nodes of every continuation's tree behind its tail and attend.
+        Q, K, V: [L][N nodes][heads][D], node i of continuation c at c nodes + i (of
+        padding, anything).  Returns O [L][H_q][N nodes][D] of the element type; it and
+        lse_nodes stay until the next draft."""
+        if self.length >= self.max_new:
+            raise ValueError(f"the tails hold {self.max_new} tokens")
+        c, N, M = self.ep.shape.c, self.fan[-1], tree.nodes
+        if tree.masks.shape[0] != N or M > self.max_nodes:
+            raise ValueError(f"trees of {tree.masks.shape[0]} continuations and {M} nodes, made for {N} and {self.max_nodes}")
+        if isinstance(K, torch.Tensor) and K.shape[-3:-2] != (N * M,):
+            raise ValueError(f"K has shape {tuple(K.shape)}, the draft has {N} x {M} nodes")
+        L, Hq, D = c.num_layers, c.num_q_heads, c.head_dim
+        n, max_tail = L * Hq * N * M, self.length if max_tail is None else max_tail
+        self.Q_nodes, self.O_nodes = (t[:n * D].view(L, Hq, N * M, D) for t in self._nodes[:2])
+        self.lse_nodes = self._nodes[2][:n].view(L, Hq, N * M)
+        self._need(E.ecokv_decode_tree_workspace_size(self.ep.shape, self.fan, self.max_count, max_tail, M), stream)
+        self._stream = stream
+        with torch.cuda.stream(stream):  # (None: the current stream stays)
+            rows, positions = self._at[0::2, :, None] + tree.steps
+        E.ecokv_append(Q, K, V, self.ep.shape, self.rope, positions, tree.conts, rows, self.tails, self.Q_nodes, stream)
+        E.ecokv_decode_tree(self.Q_nodes, self.ep.Kc, self.ep.Vc, self.ep.shape, self.fan, self.ep.counts, self.ep.offsets, self.max_count,
+                            self.tails, self.rows, max_tail, tree.masks, self.O_nodes, self.lse_nodes, self.workspace, stream)
+        self._pending, self._unweighed = "draft", None
+        return self.O_nodes
+
+    def commit(self, path: torch.Tensor, accepted: torch.Tensor, longest: Optional[int] = None, stream=None) -> None:
+        """The accepted nodes of the draft become the tails' next rows: path int32
+        [N][nodes], of which the first accepted[c] (int32 [N]) count, ascending.
+        `longest`: the rows of the longest tail afterwards or more, where the caller
+        knows better than `nodes` more than before."""
+        if self._pending != "draft":
+            raise ValueError("commit goes with a draft")
+        N, M = self.fan[-1], self.lse_nodes.shape[2] // self.fan[-1]
+        if tuple(path.shape) != (N, M):
+            raise ValueError(f"path has shape {tuple(path.shape)}, the draft has ({N}, {M}) nodes")
+        stream = self._stream if stream is None else stream
+        E.ecokv_commit(self.ep.shape, self.tails, self.rows, path, accepted, stream)
+        with torch.cuda.stream(stream):
+            self._at.add_(accepted)
+        self.length = self.length + M if longest is None else min(self.length + M, int(longest))
+        self._pending, self._unweighed = None, (path, accepted)
+
+    def accumulate(self, decay: float = 1.0, stream=None, max_tail: Optional[int] = None) -> None:
+        """Add the weights of the last step, or of the accepted nodes of the last
+        commit, to the masses, once."""
+        self._with_masses(False)
+        if self._unweighed is None:
+            raise ValueError("accumulate goes with a step or a commit, once")
+        if self._unweighed == "step":
+            Q, lse, path, accepted = self.Q_dec, self.lse, None, None
+        else:
+            Q, lse, (path, accepted) = self.Q_nodes, self.lse_nodes, self._unweighed
+        # (a step's row is the tail's last, whether it was advanced or not)
+        counts, most = (self.tail_counts, self.length + 1) if self._pending == "step" else (self.rows, self.length)
+        stream = self._stream if stream is None else stream
+        E.ecokv_accumulate(Q, lse, self.ep.Kc, self.ep.shape, self.fan, self.ep.counts, self.ep.offsets, self.max_count, self.tails, counts,
+                           most if max_tail is None else max_tail, self.mass, self.tail_mass, path, accepted, decay, stream=stream)
+        self._unweighed = None
+
+    def evict(self, limit: int, keep: int, recent: int, stream=None, max_tail: Optional[int] = None) -> None:
+        """Tails of more than `limit` rows keep `keep` of them: the last `recent`, and of
+        the others those of the largest mass."""
+        self._with_masses(True)
+        max_tail = self.length if max_tail is None else max_tail
+        stream = self._stream if stream is None else stream
+        self._need(E.ecokv_evict_workspace_size(self.ep.shape, self.fan[-1], max_tail, keep), stream)
+        E.ecokv_evict_tails(self.ep.shape, self.tails, self.rows, max_tail, limit, keep, recent, self.tail_mass,
+                            workspace=self.workspace, stream=stream)
+        with torch.cuda.stream(stream):
+            torch.add(self.rows, 1, out=self.tail_counts)
+        self.length, self._unweighed = min(self.length, limit), None
+
+    def evict_kept(self, limit: int, keep: int, recent: int, stream=None) -> None:
+        """The same for the prompts' kept rows, each (layer, KV head, prompt) on its own:
+        the pass's Kc, Vc and counts change."""
+        self._with_masses(True)
+        shape = self.ep.shape
+        stream = self._stream if stream is None else stream
+        self._need(max(E.ecokv_evict_workspace_size(shape, shape.c.num_seqs, self.max_count, keep),
+                       E.ecokv_decode_shared_workspace_size(shape, self.fan, min(self.max_count, limit), self.max_new)), stream)
+        E.ecokv_evict(self.ep.Kc, self.ep.Vc, shape, self.ep.counts, self.ep.offsets, self.max_count, limit, keep, recent, self.mass,
+                      workspace=self.workspace, stream=stream)
+        self.max_count, self._unweighed = min(self.max_count, limit), None
+
+    def _with_masses(self, between: bool) -> None:
+        if self.mass is None:
+            raise ValueError("made without masses")
+        if between and self._pending:
+            raise ValueError(f"a {self._pending} is not finished: rows are evicted between tokens")
+
+
+class Tree:
+    """Drafted trees of continuations on the device (made by Continuations.tree)."""
+
+    def __init__(self, parents, nodes: int, device):
+        masks, steps = [], [[], []]  # (row behind the tail, depth)
+        for p in parents:
+            m, depths = E.ecokv_tree_masks(p) if p else ([], [])
+            pad = nodes - len(p)
+            masks.append(m + [0] * pad)
+            steps[0].append(list(range(len(p))) + [-(1 << 30)] * pad)  # (a negative row is not written)
+            steps[1].append(depths + [0] * pad)
+        self.nodes = nodes
+        self.masks = torch.tensor(masks, dtype=torch.int64, device=device)
+        self.steps = torch.tensor(steps, dtype=torch.int32, device=device)
+        self.conts = torch.arange(len(parents), dtype=torch.int32, device=device).repeat_interleave(nodes)
