@@ -746,7 +746,10 @@ template <bool TREE>
 static hipError_t merge_launch(const SharedArgs &a, hipStream_t st)
 {
     const int parts = a.grid.np + a.grid.nt;
-    const int few = parts <= 2 ? 2 : parts <= 3 ? 3 : parts <= 5 ? 5 : parts <= 8 ? 8 : parts <= 14 ? 14 : parts <= kShFew ? kShFew : 0;
+    int few = parts <= 2 ? 2 : parts <= 3 ? 3 : parts <= 5 ? 5 : parts <= 8 ? 8 : parts <= 14 ? 14 : parts <= kShFew ? kShFew : 0;
+    // (a tree's few rows: us a whole call, a block a row and the forms above: 224 rows of 23
+    // and 24 partials 16.6 20.5, 448 of 18 and 20 20.1 23.0, 896 of 18 and 20 24.6 27.0)
+    if (TREE && a.grid.qrows <= (parts > 14 ? 1024 : parts > 5 ? 512 : 0)) few = 0;
     const int per = few ? kShMergeThreads / (a.D / 4) : 1;
     const dim3 g = blocks_grid((a.grid.qrows + per - 1) / per);
     ECOKV_TIMED(TREE ? "tree_merge" : "shared_merge", st,

@@ -157,11 +157,12 @@ __device__ __forceinline__ void wide_part(const SharedArgs &a, const SharedItem 
     load_queries<BF, D, QT>(a, it, q0, nq, w);
     put(ld, 0, ring);
     if (tiles > 2) load(ld, 1);
-    const auto step = [&](int t, int odd) {
+    const auto step = [&](int t, int odd) __attribute__((always_inline)) {
         const u32x4s *const sk = stage + odd * 2 * Ge::TILE, *const sv = sk + 4 * Ge::TILE;
         // operands are read from LDS AHEAD matrix instructions ahead (the compiler would
-        // read each just before its use, a latency of LDS for every pair)
-        constexpr int AHEAD = TWICE ? 8 : 4, NV = 4 * Ge::DT;
+        // read each just before its use, a latency of LDS for every pair; 8 ahead left some
+        // of the loop's values in scratch memory)
+        constexpr int AHEAD = TWICE ? 6 : 4, NV = 4 * Ge::DT;
         bf16x8s op[AHEAD];
         const auto kop = [&](int i) {  // 16 dimensions i / 2 of tile i % 2
             return __builtin_bit_cast(bf16x8s, sk[i % 2 * Ge::TILE + stage_chunk<BF, Ge::S>(row, 2 * (i / 2) + grp)]);
@@ -216,9 +217,9 @@ __device__ __forceinline__ void wide_part(const SharedArgs &a, const SharedItem 
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int k = i / Ge::DT, d = i % Ge::DT;
-                w.acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[i % AHEAD], __builtin_bit_cast(bf16x8s, p[k / 2][k % 2][0]), w.acc[d], 0, 0, 0);
-                if (i + AHEAD < NV) op[i % AHEAD] = vop(i + AHEAD);
+                const int k = i / Ge::DT, d = i % Ge::DT, o = (2 * Ge::QS + i) % AHEAD;
+                w.acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[o], __builtin_bit_cast(bf16x8s, p[k / 2][k % 2][0]), w.acc[d], 0, 0, 0);
+                if (i + AHEAD < NV) op[o] = vop(i + AHEAD);
                 __builtin_amdgcn_sched_barrier(0);
             }
         } else {
@@ -494,11 +495,14 @@ __global__ __launch_bounds__(kShThreads, 2) void k_tree(TreeArgs a)
 template <bool BF, int D>
 static void launch_tree(const TreeArgs &a, dim3 grid, hipStream_t st)
 {
-    const bool wide = a.s.grid.wq == 4, twide = a.tails.wq == 4;
-    if (wide && twide) hipLaunchKernelGGL((k_tree<BF, D, 4, 4>), grid, dim3(kShThreads), 0, st, a);
-    else if (wide) hipLaunchKernelGGL((k_tree<BF, D, 4, 1>), grid, dim3(kShThreads), 0, st, a);
-    else if (twide) hipLaunchKernelGGL((k_tree<BF, D, 1, 4>), grid, dim3(kShThreads), 0, st, a);
-    else hipLaunchKernelGGL((k_tree<BF, D, 1, 1>), grid, dim3(kShThreads), 0, st, a);
+    const bool wide = a.s.grid.wq == 4;
+    if (a.tails.wq == 4) {
+        if (wide) hipLaunchKernelGGL((k_tree<BF, D, 4, 4>), grid, dim3(kShThreads), 0, st, a);
+        else hipLaunchKernelGGL((k_tree<BF, D, 1, 4>), grid, dim3(kShThreads), 0, st, a);
+    } else if constexpr (!(BF && D == 128)) {
+        if (wide) hipLaunchKernelGGL((k_tree<BF, D, 4, 1>), grid, dim3(kShThreads), 0, st, a);
+        else hipLaunchKernelGGL((k_tree<BF, D, 1, 1>), grid, dim3(kShThreads), 0, st, a);
+    }
 }
 
 hipError_t tree_launch(const TreeArgs &a, bool bf16, hipStream_t st)

@@ -10,14 +10,16 @@ namespace ecokv {
 // The tails' part of a call.  A continuation has nodes x G query rows for every
 // (layer, KV head): cut into tiles of wq x rows_q; its tail and the drafted rows
 // behind it into grid.nt parts.  wq = 4: a block takes one tile and one part;
-// wq = 1 (the query rows fit one wave): a wave does.  Part k has the rows from
-// k * rows on, whatever the count.
+// wq = 1: a wave does.  Part k has the rows from k * rows on, whatever the count.
 struct TreeTails {
     int wq, tiles, rows;
     int64_t blocks;
 };
 
-constexpr int kTreeRows = 512;  // rows of a prompt's part that are worth a block of its own
+// Rows of a prompt's part that are worth a block of its own, in wide and in narrow
+// tiles (us, 28 query rows of 4 heads, 1500 kept rows in parts of 768, 384 and 256: 15.7
+// 13.5 13.6; 6553 in parts of 640, 480 and 384: 15.5 14.7 14.3).
+constexpr int kTreeRows = 512, kTreeNarrowRows = 256;
 
 // fan counts nodes (fan[s + 1] - fan[s] of prompt s); conts continuations.
 inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *fan, int conts, int nodes, int max_count,
@@ -41,7 +43,12 @@ inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *f
     g.tiles = max_count > 0 ? g.tile0[B] : 0;
     g.qrows = pairs * G * fan[B];
     const int rows = max_tail + nodes;
-    tails->wq = nodes * G <= g.rows_q ? 1 : 4;
+    // A wave of its own for query rows that fit one, but not with 128-wide bf16 rows: its
+    // loads, tile and sums need 61 registers more than there are (us, four waves and one:
+    // 28 query rows of 4 heads and 704 rows 15.5 23.7, 28 layers of them 91 109, 8 layers of
+    // 8000 rows 58 64; 128 heads of 24 query rows and 4000 rows 99 95; 64-wide, 1000 rows
+    // 23.4 21.6, 8000 rows 98 66; fp32 of 6 such answers, 28 layers, 1000 rows 154 96).
+    tails->wq = nodes * G <= g.rows_q && !(bf16 && D == 128) ? 1 : 4;
     const int tt = tails->wq * g.rows_q;
     tails->tiles = (nodes * G + tt - 1) / tt;
     const int64_t have = pairs * conts * tails->tiles;  // (continuation, tile)s
@@ -49,7 +56,16 @@ inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *f
     const int64_t prompt_have = pairs * g.tiles, tail_least = tails->wq == 1 ? (have + kShWaves - 1) / kShWaves : have;
 
     g.np = prompt_parts(g, prompt_have, pairs * prompts, D, max_count, bf16);
-    if (g.wq == 4 && g.np > 0) {
+    if (g.wq == 1 && g.np > 0) {
+        // no shorter parts, and no block that shares its compute unit with a tail's,
+        // where that takes few parts away (us, 112 query rows of 4 heads, 6553 kept rows,
+        // 12 and 16 parts beside 24 blocks of tails: 20.0 22.6)
+        const int64_t most = (max_count + kTreeNarrowRows - 1) / kTreeNarrowRows;
+        const int64_t tails_most = tail_least * ((rows + 4 * g.rows_t - 1) / (4 * g.rows_t)), room = (kShBlocks - tails_most) / prompt_have;
+        int64_t np = g.np < most ? g.np : most;
+        if (room < np && 4 * room >= 3 * np) np = room;
+        g.np = parts_within(np, max_count, g.step);
+    } else if (g.np > 0) {
         // two blocks per compute unit where the parts stay long
         const int64_t fill = (slots - tail_least) / prompt_have, most = max_count / kTreeRows;
         const int64_t np = fill < most ? fill : most;
@@ -62,26 +78,28 @@ inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *f
         g.tail_step = 2 * g.rows_t;
         const int64_t one = kShBlocks * kShWaves / have, two = 2 * kShBlocks * kShWaves / have;
         g.nt = parts_within(two > one && rows / two >= 256 ? two : one < 1 ? 1 : one, rows, g.tail_step);
-        g.tail_waves = have * g.nt;
-        tails->blocks = (g.tail_waves + kShWaves - 1) / kShWaves;
     } else {
         // as many as there is room for beside the prompts, none short, and none longer
-        // than a prompt's part
+        // than a prompt's part (nor cut where that is short: 22 tails of 1810 rows beside
+        // 22 x 76 kept rows took 100 us in 24 parts, 50 in 4)
         g.tail_step = 2 * g.rows_t;
         int64_t nt;
         if (g.np > 0) {
-            const int64_t like = ((int64_t)max_count + g.np - 1) / g.np, least = (rows + like - 1) / like;
-            const int64_t room = (slots - g.prompt_blocks) / have, most = rows / (4 * g.rows_t);
+            int64_t like = ((int64_t)max_count + g.np - 1) / g.np;
+            like = like < kTreeRows ? kTreeRows : like;
+            const int64_t least = (rows + like - 1) / like;
+            const int64_t room = (slots - g.prompt_blocks) / have, most = (rows + 4 * g.rows_t - 1) / (4 * g.rows_t);
             nt = room < most ? room : most;
             nt = nt > least ? nt : least;
         } else {
             nt = prompt_parts(g, have, pairs * conts, D, rows, bf16);
         }
         g.nt = parts_within(nt < 1 ? 1 : nt, rows, g.tail_step);
-        g.tail_waves = 0;
-        tails->blocks = have * g.nt;
     }
     tails->rows = (int)part_rows(rows, g.nt, g.tail_step);
+    g.nt = parts_used(rows, g.nt, g.tail_step);  // (rounded up, fewer may do)
+    g.tail_waves = tails->wq == 1 ? have * g.nt : 0;
+    tails->blocks = tails->wq == 1 ? (g.tail_waves + kShWaves - 1) / kShWaves : have * g.nt;
     g.bytes = sizeof(float) * (size_t)(g.np + g.nt) * (size_t)g.qrows * (size_t)(D + 2);
     return g;
 }
