@@ -43,6 +43,7 @@ inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *f
     g.tiles = max_count > 0 ? g.tile0[B] : 0;
     g.qrows = pairs * G * fan[B];
     const int rows = max_tail + nodes;
+    const int64_t short_parts = ((int64_t)rows + 4 * g.rows_t - 1) / (4 * g.rows_t);  // of four tiles
     // A wave of its own for query rows that fit one, but not with 128-wide bf16 rows: its
     // loads, tile and sums need 61 registers more than there are (us, four waves and one:
     // 28 query rows of 4 heads and 704 rows 15.5 23.7, 28 layers of them 91 109, 8 layers of
@@ -60,8 +61,8 @@ inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *f
         // no shorter parts, and no block that shares its compute unit with a tail's,
         // where that takes few parts away (us, 112 query rows of 4 heads, 6553 kept rows,
         // 12 and 16 parts beside 24 blocks of tails: 20.0 22.6)
-        const int64_t most = (max_count + kTreeNarrowRows - 1) / kTreeNarrowRows;
-        const int64_t tails_most = tail_least * ((rows + 4 * g.rows_t - 1) / (4 * g.rows_t)), room = (kShBlocks - tails_most) / prompt_have;
+        const int64_t most = ((int64_t)max_count + kTreeNarrowRows - 1) / kTreeNarrowRows;
+        const int64_t room = (kShBlocks - tail_least * short_parts) / prompt_have;
         int64_t np = g.np < most ? g.np : most;
         if (room < np && 4 * room >= 3 * np) np = room;
         g.np = parts_within(np, max_count, g.step);
@@ -88,8 +89,8 @@ inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *f
             int64_t like = ((int64_t)max_count + g.np - 1) / g.np;
             like = like < kTreeRows ? kTreeRows : like;
             const int64_t least = (rows + like - 1) / like;
-            const int64_t room = (slots - g.prompt_blocks) / have, most = (rows + 4 * g.rows_t - 1) / (4 * g.rows_t);
-            nt = room < most ? room : most;
+            const int64_t room = (slots - g.prompt_blocks) / have;
+            nt = room < short_parts ? room : short_parts;
             nt = nt > least ? nt : least;
         } else {
             nt = prompt_parts(g, have, pairs * conts, D, rows, bf16);

@@ -175,3 +175,17 @@ def test_workspaces_that_were_outgrown_are_kept(rec):
     assert co.workspace is first
     co._need(first.numel() + 1, None)
     assert co.workspace is not first and co._outgrown == [first]
+
+
+def test_a_draft_has_the_workspace_it_needs(rec):
+    # shorter tails may be split otherwise and need more than the longest
+    import paper_2609_06663_amd as P
+    from paper_2609_06663_amd.pipeline import Continuations, EvictionPass
+    ep = EvictionPass(P.Shape(1, 28, 4, 128, 4, [0, 9000]), [6553], device="cpu")
+    co = Continuations(ep, [1], 20000, P.Rope(0), 64, 64)
+    t = co.tree([-1] * 64)
+    for length in (0, 296, 333, 5000, 19999):
+        co.length = length
+        co.draft(*(torch.zeros(1, 64, h, 128) for h in (28, 4, 4)), t)
+        assert rec.calls[-1][0] == "decode_tree" and rec.calls[-1][1][10] == length
+        assert rec.calls[-1][1][14].numel() >= P.ecokv_decode_tree_workspace_size(ep.shape, co.fan, co.max_count, length, 64)

@@ -103,21 +103,6 @@ def test_tree_parts_cover_every_row_once(lib, G, nodes):
                         assert rc == 0, (rc, pairs, fan, mc, mt, bf16, D, out.tolist())
 
 
-def test_more_rows_of_tails_need_no_less(lib):
-    # (Continuations sizes its workspace for the longest tails first)
-    out = np.zeros(6, np.int64)
-    n = np.zeros(1, np.int32)
-    for pairs, G, fan, nodes, mc in ((4, 7, [1], 64, 6553), (112, 7, [8], 16, 6553), (8, 4, [5, 1, 6], 13, 4480), (32, 1, [4], 24, 1500), (2, 2, [1], 5, 100)):
-        conts = np.concatenate([[0], np.cumsum(fan)])
-        cum = (nodes * conts).astype(np.int32)
-        for bf16 in (0, 1):
-            before = 0
-            for mt in range(0, 20000, 37):
-                assert lib.tree(pairs, G, 128, len(fan), cum.ctypes.data, int(conts[-1]), nodes, mc, mt, bf16, n.ctypes.data, 0, out.ctypes.data) == 0
-                assert out[4] >= before, (pairs, fan, mt)
-                before = out[4]
-
-
 def test_pieces_of_masses(lib):
     out = np.zeros(4, np.int64)
     for pairs in (1, 4, 112, 2000):
