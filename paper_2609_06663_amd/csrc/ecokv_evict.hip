@@ -21,8 +21,8 @@ constexpr int kCommitThreads = 256;
 // registers hold, all of these read before the first is written.  Most units have a few
 // rows, so the time is a chain of four loads (accepted, path, page, row): a wave each and
 // not a block lets more run at once (28 layers of 48 continuations, 15 rows each on
-// average, us: a block for K and one for V 22.9, a wave each 17.0, a wave for both 16.5,
-// 82 MB at 5.0 TB/s).
+// average, us a call: a block for K and one for V 22.9, a wave each 20.2, a wave for both
+// 19.0, rows stored past the L2 16.4, which is 79 MB at 4.8 TB/s).
 template <int S>
 __global__ __launch_bounds__(kCommitThreads) void k_commit(CommitArgs a)
 {
@@ -69,8 +69,8 @@ __global__ __launch_bounds__(kCommitThreads) void k_commit(CommitArgs a)
             const int r = __shfl(to, k, kWave), page = __shfl(pt, k, kWave);
             const int64_t at = tail_row(a.map, a.Hkv, l, h, page, r) * (16 * S) + 16 * (j % S);
             if (j < chunks) {
-                *reinterpret_cast<u32x4e *>(a.K + at) = x[0][i];
-                *reinterpret_cast<u32x4e *>(a.V + at) = x[1][i];
+                __builtin_nontemporal_store(x[0][i], reinterpret_cast<u32x4e *>(a.K + at));
+                __builtin_nontemporal_store(x[1][i], reinterpret_cast<u32x4e *>(a.V + at));
             }
         }
     }
@@ -457,7 +457,9 @@ __device__ __forceinline__ void move_masses(const EvictArgs &a, const EvictUnit 
 }
 
 // A block moves the chunks [c0, c0 + cols) of 16 bytes of a unit's rows, K's and V's
-// side by side; one more block per unit the masses.
+// side by side; one more block per unit the masses.  Rows are stored past the L2, which
+// their loads then have to themselves (us a call, 28 layers of 16 tails of 1152 rows 121
+// and 114, 160 units of 6553 rows 63.5 and 56.2; loads past it as well: 110 and 60.3).
 __global__ __launch_bounds__(kMoveThreads) void k_evict_move(EvictArgs a)
 {
     const uint32_t b = blockIdx.z * (uint32_t)kGridX + blockIdx.x;
@@ -501,7 +503,7 @@ __global__ __launch_bounds__(kMoveThreads) void k_evict_move(EvictArgs a)
         number(src, i + step, from2), number(dst, i + step, to2);
 #pragma unroll
         for (int j = 0; j < U; ++j) {
-            if (i + j * per + mine < moves) *row(to[j]) = v[j];
+            if (i + j * per + mine < moves) __builtin_nontemporal_store(v[j], row(to[j]));
             from[j] = from2[j], to[j] = to2[j];
         }
     }
@@ -525,7 +527,7 @@ __global__ __launch_bounds__(kMoveThreads) void k_evict_move(EvictArgs a)
         if (i + step < a.recent) load(w, i + step);
 #pragma unroll
         for (int j = 0; j < U; ++j) {
-            if (i + j * per + mine < a.recent) *row(heavy + i + j * per + mine) = v[j];
+            if (i + j * per + mine < a.recent) __builtin_nontemporal_store(v[j], row(heavy + i + j * per + mine));
             v[j] = w[j];
         }
     }
