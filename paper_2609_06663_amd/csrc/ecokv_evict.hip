@@ -22,7 +22,7 @@ constexpr int kCommitThreads = 256;
 // rows, so the time is a chain of four loads (accepted, path, page, row): a wave each and
 // not a block lets more run at once (28 layers of 48 continuations, 15 rows each on
 // average, us a call: a block for K and one for V 22.9, a wave each 20.2, a wave for both
-// 19.0, rows stored past the L2 16.4, which is 79 MB at 4.8 TB/s).
+// 19.0, rows stored past the L2 16.4, which is 77 MB at 4.6 TB/s).
 template <int S>
 __global__ __launch_bounds__(kCommitThreads) void k_commit(CommitArgs a)
 {

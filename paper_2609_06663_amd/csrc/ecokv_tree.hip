@@ -3,9 +3,10 @@
 // behind it.
 //
 // A prompt's kept rows are read by nodes x continuations x G query rows of a
-// (layer, KV head): that part is ecokv_decode_shared's, a node in the place of a
-// continuation (prompt_part).  A continuation's tail and drafted rows are read by
-// its nodes x G query rows: the same tiles, rows found page by page.  Node i sees
+// (layer, KV head), a node in the place of ecokv_decode_shared's continuation: tiles of
+// 32 query rows, a wave each (prompt_part), or of 128, whose four waves share the rows
+// (wide_part).  A continuation's tail and drafted rows are read by its nodes x G query
+// rows: the same tiles, rows found page by page (tree_part).  Node i sees
 // drafted row j where bit j of its mask is set, so a lane, which has one query
 // row, masks the logits of its node; only tiles with drafted rows (or the last
 // rows) are masked at all.  Partials are joined by k_shared_merge.
