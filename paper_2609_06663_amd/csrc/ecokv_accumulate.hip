@@ -67,7 +67,8 @@ __global__ __launch_bounds__(kMassThreads, BF ? 4 : 3) void k_mass(MassArgs a)
     __shared__ uint16_t list[kMassList];              // nodes, counted from the first listed continuation's; 65535: none
     __shared__ u32x4m qs[kMassTiles][Ge::ST][kWave];  // 16 query rows each, in the order of the operands
     __shared__ float zs[2][16 * kMassTiles];          // z, and what its roundings leave out
-    __shared__ int lasts[16 * kMassTiles];            // the last row of the tail that a query sees
+    __shared__ int lasts[16 * kMassTiles];            // the last row of the tail that a query sees; INT32_MIN: it weighs nothing
+    __shared__ int voids[kMassTiles];                 // whether a tile has such queries
     const uint32_t b = blockIdx.z * (uint32_t)kGridX + blockIdx.x;
     const int lane = threadIdx.x & 63, wv = uniform_i32(threadIdx.x >> 6), grp = lane >> 4, row16 = lane & 15;
     const bool tail = b >= (uint32_t)a.kept_blocks;
@@ -143,14 +144,16 @@ __global__ __launch_bounds__(kMassThreads, BF ? 4 : 3) void k_mass(MassArgs a)
             float lse = a.lse[qrow];
 #pragma unroll
             for (int s = 0; s < Ge::ST; ++s) qs[qt][s][lane] = q[s];
-            // a query that is not there, or that saw no row, weighs nothing
-            if (none || q0 + row16 >= queries || lse == -INFINITY) lse = INFINITY;
+            // a query that is not there, or that saw no row, weighs nothing, whatever it holds
+            const bool nothing = none || q0 + row16 >= queries || lse == -INFINITY;
+            const bool odd = __builtin_amdgcn_ballot_w64(nothing) != 0;
+            if (lane == 0) voids[qt] = odd;
             constexpr float kLog2e = 1.44269504f, kLog2eRest = 1.92596299e-8f;
             const float z = lse * kLog2e;
             if (grp == 0) {
                 zs[0][16 * qt + row16] = z;
                 zs[1][16 * qt + row16] = fabsf(z) < INFINITY ? z * a.scale_rest - fmaf(lse, kLog2eRest, fmaf(lse, kLog2e, -z)) : 0.f;
-                lasts[16 * qt + row16] = tail ? n - fresh + p : 0;
+                lasts[16 * qt + row16] = nothing ? INT32_MIN : tail ? n - fresh + p : 0;
             }
         }
         __syncthreads();
@@ -199,12 +202,18 @@ __global__ __launch_bounds__(kMassThreads, BF ? 4 : 3) void k_mass(MassArgs a)
                     for (int s = 0; s < Ge::ST; ++s) q[s] = qs[qt][s][lane];
                     const float z = zs[0][16 * qt + row16], dz = zs[1][16 * qt + row16];
                     const int last = lasts[16 * qt + row16];
+                    const bool odd = uniform_i32(voids[qt]) != 0;
 #pragma unroll
                     for (int t = 0; t < RT; ++t) {
                         const f32x4m x = mass_logits<BF, D>(k[t], q);
                         float w[4];
 #pragma unroll
                         for (int r = 0; r < 4; ++r) w[r] = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale, -z) + dz);
+                        if (odd) {  // (a branch: few tiles have such)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (last == INT32_MIN) w[r] = 0.f;
+                        }
                         if (cut) {
 #pragma unroll
                             for (int r = 0; r < 4; ++r)

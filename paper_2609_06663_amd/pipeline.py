@@ -390,4 +390,4 @@ class Tree:
         self.nodes = nodes
         self.masks = torch.tensor(masks, dtype=torch.int64, device=device)
         self.steps = torch.tensor(steps, dtype=torch.int32, device=device)
-        self.conts = torch.arange(len(parents), dtype=torch.int32, device=device).repeat_interleave(nodes)
+        self.conts = torch.tensor([c for c in range(len(parents)) for _ in range(nodes)], dtype=torch.int32, device=device)

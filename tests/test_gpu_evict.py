@@ -188,6 +188,35 @@ def test_accumulate_edges():
     assert float(mo[3]) == float(t3.mass[3]) and bool(mo[4].isnan()) and int(mo.isnan().sum()) == 1
 
 
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 128)])
+def test_accumulate_queries_that_weigh_nothing(dtype, D):
+    """Whatever a query holds that a path leaves out, that saw no row or that only fills a tile."""
+    say(f"accumulate, queries that weigh nothing {dtype} {D}")
+    t = Masses(11, dtype, 1, 4, 2, D, [[[90], [80]]], [3], [40, 41, 9], 5, page=8, accepted=[2, 3, 0])
+    want = t.run(0.5)
+    t.check(*want, 0.5)
+    t.path_t[0, 2], t.path_t[1, 3], t.path_t[2, 0] = 5, -1, 99           # not accepted: not read
+    t.acc_t[0], t.acc_t[1] = 3, 4
+    for c, k in ((0, 2), (1, 3)):                                      # accepted, not there
+        t.path[c], t.acc[c] = t.path[c][:k], k
+    used = {c * 5 + v for c in range(3) for v in t.path[c][:t.acc[c]]}
+    for q in set(range(15)) - used:
+        t.Q[:, :, q], t.lse[:, :, q] = float("nan"), float("inf")
+    got = t.run(0.5)
+    t.check(*got, 0.5, skip_conts=(0, 1))                                # (the sums' order is another)
+    # a node that saw no row: its query does not matter either
+    gone = t.path[1][1]
+    t.lse[:, :, 5 + gone] = -float("inf")
+    clean = t.run(0.5)[0]
+    t.Q[:, :, 5 + gone] = float("nan")
+    got = t.run(0.5)[0]
+    assert torch.equal(got, clean) and not torch.equal(got, want[0]) and bool(got[:170].isfinite().all())
+    # and where rows hold infinities, so that products with nothing are NaN
+    t.Kc[5, 3] = float("inf")
+    got = t.run(0.5)[0]
+    assert not bool(got.isnan().any()) and torch.equal(torch.cat([got[:5], got[6:170]]), torch.cat([clean[:5], clean[6:170]]))
+
+
 def test_accumulate_without_continuations():
     """Prompts that nobody continues only fade."""
     say("accumulate, no continuations")
