@@ -723,6 +723,53 @@ __global__ __launch_bounds__(kShMergeThreads) void k_shared_merge(SharedArgs a)
     }
 }
 
+// A tree's 9 to 32 partials: a wave per query row.  16 lanes share the row's D sums, and
+// the four groups of them take every fourth partial, up to PER, all loaded at once, and
+// join by lane moves: an eighth of the loads of a lane of the forms above (us a whole
+// call, those forms and this: 1792 rows of 10 partials 28.2 26.9, 896 of 13 21.6 20.1,
+// 64-wide 3072 of 18 66.2 63.6; of 6 to 8 partials 106.1 108.5, 111.7 112.7, 60.3 59.4).
+template <int D, int PER>
+__global__ __launch_bounds__(kShMergeThreads) void k_shared_merge_wave(SharedArgs a)
+{
+    constexpr int C = D / 64;  // sums of a lane, by fours
+    const uint32_t qrow = (blockIdx.z * (uint32_t)kGridX + blockIdx.x) * (kShMergeThreads / kWave) + (uint32_t)uniform_i32(threadIdx.x >> 6);
+    if (qrow >= (uint32_t)a.grid.qrows) return;
+    const int lane = threadIdx.x & 63, d = 4 * C * (lane & 15), grp = lane >> 4, P = a.grid.np + a.grid.nt;
+    f32x4s v[PER][C];
+    float2 e[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int64_t row = (int64_t)min(grp + 4 * k, P - 1) * a.grid.qrows + qrow;
+        e[k] = a.ms[row];
+#pragma unroll
+        for (int c = 0; c < C; ++c) v[k][c] = *reinterpret_cast<const f32x4s *>(a.acc + row * D + d + 4 * c);
+    }
+    const ShParts r = row_parts<true>(a, qrow);
+    float M = -INFINITY, L = 0.f;
+    f32x4s o[C] = {};
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+        if (grp + 4 * k < P && has_part(a, r, grp + 4 * k)) M = fmaxf(M, e[k].x);
+    M = across32(across16(M, OpMax{}), OpMax{});
+    const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+        if (grp + 4 * k < P && has_part(a, r, grp + 4 * k)) {
+            const float w = exp2f(e[k].x - ref);
+            L += e[k].y * w;
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[c] += v[k][c] * w;
+        }
+    L = across32(across16(L, OpAdd{}), OpAdd{});
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[c][i] = across32(across16(o[c][i], OpAdd{}), OpAdd{});
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        if (grp == c) write_out<true>(a, qrow, d + 4 * c, r.bad, M, L, o[c]);
+}
+
 template <int D, bool TREE>
 static void launch_merge(const SharedArgs &a, int few, dim3 grid, hipStream_t st)
 {
@@ -731,9 +778,14 @@ static void launch_merge(const SharedArgs &a, int few, dim3 grid, hipStream_t st
     else if (few == 3) hipLaunchKernelGGL((k_shared_merge_few<D, 3, TREE>), grid, b, 0, st, a);
     else if (few == 5) hipLaunchKernelGGL((k_shared_merge_few<D, 5, TREE>), grid, b, 0, st, a);
     else if (few == 8) hipLaunchKernelGGL((k_shared_merge_few<D, 8, TREE>), grid, b, 0, st, a);
-    else if (few == 14) hipLaunchKernelGGL((k_shared_merge_few<D, 14, TREE>), grid, b, 0, st, a);
-    else if (few == kShFew) hipLaunchKernelGGL((k_shared_merge_few<D, kShFew, TREE>), grid, b, 0, st, a);
-    else hipLaunchKernelGGL((k_shared_merge<D, TREE>), grid, b, 0, st, a);
+    else if (few == 0) hipLaunchKernelGGL((k_shared_merge<D, TREE>), grid, b, 0, st, a);
+    else if constexpr (TREE) {
+        if (few == 16) hipLaunchKernelGGL((k_shared_merge_wave<D, 4>), grid, b, 0, st, a);
+        else hipLaunchKernelGGL((k_shared_merge_wave<D, 8>), grid, b, 0, st, a);
+    } else {
+        if (few == 14) hipLaunchKernelGGL((k_shared_merge_few<D, 14, TREE>), grid, b, 0, st, a);
+        else hipLaunchKernelGGL((k_shared_merge_few<D, kShFew, TREE>), grid, b, 0, st, a);
+    }
 }
 
 inline dim3 blocks_grid(int64_t n)
@@ -747,10 +799,13 @@ static hipError_t merge_launch(const SharedArgs &a, hipStream_t st)
 {
     const int parts = a.grid.np + a.grid.nt;
     int few = parts <= 2 ? 2 : parts <= 3 ? 3 : parts <= 5 ? 5 : parts <= 8 ? 8 : parts <= 14 ? 14 : parts <= kShFew ? kShFew : 0;
-    // (a tree's few rows: us a whole call, a block a row and the forms above: 224 rows of 23
-    // and 24 partials 16.6 20.5, 448 of 18 and 20 20.1 23.0, 896 of 18 and 20 24.6 27.0)
-    if (TREE && a.grid.qrows <= (parts > 14 ? 1024 : parts > 5 ? 512 : 0)) few = 0;
-    const int per = few ? kShMergeThreads / (a.D / 4) : 1;
+    int per = few ? kShMergeThreads / (a.D / 4) : 1;
+    if (TREE && parts > 5) {
+        // (of so few rows a block each: us a whole call, the next form and this, 224 rows of 23
+        // partials 17.4 16.8, 112 of 30 15.1 14.5)
+        if (a.grid.qrows <= 256 || parts > 32) few = 0, per = 1;
+        else if (parts > 8) few = parts <= 16 ? 16 : 32, per = kShMergeThreads / kWave;
+    }
     const dim3 g = blocks_grid((a.grid.qrows + per - 1) / per);
     ECOKV_TIMED(TREE ? "tree_merge" : "shared_merge", st,
                 (a.D == 128 ? launch_merge<128, TREE>(a, few, g, st) : launch_merge<64, TREE>(a, few, g, st)));

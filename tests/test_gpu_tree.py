@@ -165,6 +165,19 @@ def test_tree_as_in_large_calls(case):
     t.check(*t.run(max_count=3_000_000))
 
 
+@pytest.mark.parametrize("dtype,D,nodes", [("bf16", 128, 24), ("bf16", 64, 40), ("bf16", 128, 3), ("f32", 128, 24), ("f32", 64, 24)])
+def test_any_number_of_parts(dtype, D, nodes):
+    """Bounds from the counts up to many times them: one part of a tail to more than 32, few of them with rows."""
+    import paper_2609_06663_amd as P
+    t = Trees(21, dtype, 1, 8, 2, D, [[[40], [300]]], [2], [40, 3], nodes, page=16, spare=9000)
+    seen = set()
+    for most in (40, 100, 150, 200, 300, 400, 600, 900, 1200, 1700, 2500, 4000, 9000):
+        say(f"{dtype} {D} {nodes}: tails of up to {most} rows")
+        t.check(*t.run(max_tail=most))
+        seen.add(P.ecokv_decode_tree_workspace_size(t.shape, t.fan, t.max_count, most, nodes) // (8 * 2 * nodes * 4 * (D + 2)))
+    assert min(seen) <= 5 and max(seen) > 32 and len(seen) > 6
+
+
 @pytest.mark.parametrize("dtype,D,Hq,Hkv,nodes", [("bf16", 128, 28, 4, 9), ("bf16", 64, 4, 4, 64), ("f32", 128, 6, 2, 3), ("f32", 64, 8, 1, 20)])
 def test_tails_alone(dtype, D, Hq, Hkv, nodes):
     say(f"tails alone {dtype} {D} {nodes}")
