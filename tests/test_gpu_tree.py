@@ -165,6 +165,41 @@ def test_tree_as_in_large_calls(case):
     t.check(*t.run(max_count=3_000_000))
 
 
+@pytest.mark.parametrize("dtype,D,L,Hq,Hkv,nodes,fan", [
+    ("bf16", 128, 1, 32, 8, 13, [5, 1, 6, 2, 0]),
+    ("bf16", 64, 3, 8, 4, 30, [1, 0, 2, 1, 1]),
+    ("bf16", 128, 1, 28, 4, 3, [9, 30, 4, 1, 2]),
+    ("f32", 128, 1, 16, 4, 7, [4, 2, 1, 3, 1]),
+    ("f32", 64, 2, 6, 2, 20, [1, 1, 2, 0, 1]),
+])
+def test_prompts_of_different_lengths(dtype, D, L, Hq, Hkv, nodes, fan):
+    """Long and short units, units without rows, bounds far above the counts."""
+    say(f"different lengths {dtype} {D} {L} {Hq}/{Hkv} {nodes} {fan}")
+    counts = [[[4480 - 97 * (h + l), 3 * h, 619 + h, max(0, 2610 - 900 * h), 1] for h in range(Hkv)] for l in range(L)]
+    t = Trees(23, dtype, L, Hq, Hkv, D, counts, fan, [7 * c % 50 for c in range(sum(fan))], nodes, page=16)
+    for bound in (4480, 20_000, 300_000):
+        O, lse = t.run(max_count=bound)
+        t.check(O, lse)
+        again = t.run(max_count=bound)
+        assert torch.equal(O, again[0]) and torch.equal(lse, again[1])
+    # lengths change between calls: nothing of the last one's split stays
+    c = t.counts.clone()
+    t.counts.copy_(torch.where(torch.arange(len(c), device="cuda") % 3 == 0, c // 5, c))
+    t.check(*t.run(max_count=20_000))
+    t.counts.zero_()
+    t.check(*t.run(max_count=20_000))
+    t.counts.copy_(c)
+    t.counts[0], t.counts[7] = 20_001, -1     # head 0's prompt 0, head 1's prompt 2
+    O, lse = t.run(max_count=20_000)
+    G, bad = Hq // Hkv, []
+    for h, s in ((0, 0), (1, 2)):
+        for k in range(t.fan[s], t.fan[s + 1]):
+            at = (0, slice(h * G, (h + 1) * G), slice(k * nodes, (k + 1) * nodes))
+            assert bool(O[at].isnan().all()) and bool(lse[at].isnan().all())
+            bad.append(k)
+    t.check(O, lse, skip=bad)
+
+
 @pytest.mark.parametrize("dtype,D,nodes", [("bf16", 128, 24), ("bf16", 64, 40), ("bf16", 128, 3), ("f32", 128, 24), ("f32", 64, 24)])
 def test_any_number_of_parts(dtype, D, nodes):
     """Bounds from the counts up to many times them: one part of a tail to more than 32, few of them with rows."""
