@@ -1240,10 +1240,11 @@ int ecokv_decode_tree_workspace_size(const ecokv_shape *shape, const int32_t *fa
     if ((rc = check_tree(si, fan, max_count, max_tail, num_nodes, nodes))) return rc;
     if (!bytes) return fail(ECOKV_EINVAL, "bytes is NULL");
     ecokv::TreeTails tails;
+    ecokv::TreeEven even;
     *bytes = 0;
     for (int bf16 = 0; bf16 < 2; ++bf16) {  // the element type changes the split; report the larger
         const size_t n = ecokv::tree_grid((int64_t)si.L * si.Hkv, si.G, si.D, si.B, nodes, fan[si.B], num_nodes, max_count,
-                                          max_tail, bf16 != 0, &tails).bytes;
+                                          max_tail, bf16 != 0, &tails, &even).bytes;
         if (n > *bytes) *bytes = n;
     }
     return ECOKV_OK;
@@ -1279,7 +1280,7 @@ int ecokv_decode_tree(const void *Q_dec, const void *Kc, const void *Vc, int dty
             return fail(ECOKV_EINVAL, "O, lse or the workspace overlaps Q_dec or the tails");
     if (overlap(so, sl) || overlap(so, sw) || overlap(sl, sw)) return fail(ECOKV_EINVAL, "O, lse and the workspace overlap");
     s.grid = ecokv::tree_grid((int64_t)si.L * si.Hkv, si.G, si.D, si.B, s.fan, fan[si.B], num_nodes, max_count, max_tail, bf16,
-                              &a.tails);
+                              &a.tails, &a.even);
     if (s.grid.prompt_blocks > INT32_MAX - (1 << 20) || s.grid.tail_waves > INT32_MAX - (1 << 20) ||
         a.tails.blocks > INT32_MAX - (1 << 20) - s.grid.prompt_blocks)
         return fail(ECOKV_EINVAL, "too many parts of kept rows or tails");
@@ -1299,6 +1300,7 @@ int ecokv_decode_tree(const void *Q_dec, const void *Kc, const void *Vc, int dty
     s.lse = lse;
     s.acc = static_cast<float *>(workspace);
     s.ms = reinterpret_cast<float2 *>(s.acc + (size_t)(s.grid.np + s.grid.nt) * (size_t)s.grid.qrows * si.D);
+    s.part_steps = a.even.fill ? reinterpret_cast<int *>(s.ms + (size_t)(s.grid.np + s.grid.nt) * (size_t)s.grid.qrows) : nullptr;
     s.L = si.L;
     s.Hq = si.Hq;
     s.Hkv = si.Hkv;

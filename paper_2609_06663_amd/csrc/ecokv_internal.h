@@ -258,7 +258,9 @@ struct SharedArgs {
     // ecokv_decode_tree: the nodes of a continuation's tree and whether O is bf16.
     // Q, O, N, fan and grid.tile0 are of nodes there, the tails' counts and tables
     // of continuations; tree_rows: TreeTails::rows.
+    // part_steps: the length of a prompt's part where TreeEven gives it, else NULL.
     int nodes, bf16, tree_rows;
+    int *part_steps;
 };
 hipError_t shared_launch(SharedArgs a, bool bf16, hipStream_t st);
 
@@ -268,6 +270,7 @@ struct TreeArgs {
     const unsigned long long *masks;  // [conts][nodes]
     int conts;
     TreeTails tails;
+    TreeEven even;
 };
 hipError_t tree_launch(const TreeArgs &a, bool bf16, hipStream_t st);
 

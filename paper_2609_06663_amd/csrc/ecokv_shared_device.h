@@ -576,7 +576,12 @@ __device__ __forceinline__ ShParts row_parts(const SharedArgs &a, uint32_t qrow)
         while (s + 1 < a.B && a.fan[s + 1] <= c) ++s;
         const int n = a.counts[(int64_t)lh * a.B + s];
         r.bad = n < 0 || n > a.max_count;
-        r.np = r.bad ? 0 : parts_used(n, a.grid.np, a.grid.step);
+        if (TREE && a.part_steps) {
+            const uint32_t step = 2 * (uint32_t)a.grid.rows_t, steps = ((uint32_t)n + step - 1) / step, each = (uint32_t)a.part_steps[0];
+            r.np = r.bad ? 0 : (int)((steps + each - 1) / each);
+        } else {
+            r.np = r.bad ? 0 : parts_used(n, a.grid.np, a.grid.step);
+        }
     }
     if (TREE || a.max_tail > 0) {  // (a tree's drafted rows are behind the tail's)
         const int n = a.tail_counts[TREE ? c / a.nodes : c];
@@ -737,14 +742,19 @@ __global__ __launch_bounds__(kShMergeThreads) void k_shared_merge_wave(SharedArg
     const int lane = threadIdx.x & 63, d = 4 * C * (lane & 15), grp = lane >> 4, P = a.grid.np + a.grid.nt;
     f32x4s v[PER][C];
     float2 e[PER];
+    ShParts r{0, 0, false};
+    const bool first = a.part_steps != nullptr;  // (half of the places are spare: only those used are read)
+    if (first) r = row_parts<true>(a, qrow);
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-        const int64_t row = (int64_t)min(grp + 4 * k, P - 1) * a.grid.qrows + qrow;
+        const int i = grp + 4 * k;
+        const int64_t row = (int64_t)min(i, P - 1) * a.grid.qrows + qrow;
+        if (first && !(i < P && has_part(a, r, i))) continue;
         e[k] = a.ms[row];
 #pragma unroll
         for (int c = 0; c < C; ++c) v[k][c] = *reinterpret_cast<const f32x4s *>(a.acc + row * D + d + 4 * c);
     }
-    const ShParts r = row_parts<true>(a, qrow);
+    if (!first) r = row_parts<true>(a, qrow);
     float M = -INFINITY, L = 0.f;
     f32x4s o[C] = {};
 #pragma unroll

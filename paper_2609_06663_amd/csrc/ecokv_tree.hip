@@ -63,6 +63,77 @@ __device__ __forceinline__ void tree_item(const TreeArgs &a, uint32_t w, TreeIte
     it.rows = valid ? uniform_i32(max(min(n + a.s.nodes - it.row0, a.tails.rows), 0)) : 0;
 }
 
+// The b-th of a call's prompt blocks where parts go by the counts (TreeEven): every wave
+// takes four units a lane, their steps' sum and the most, and with a part's length the
+// blocks of each.  Returns whether there is such a block; `each`: a part's steps.
+template <class Run>
+__device__ __forceinline__ bool even_item(const TreeArgs &a, uint32_t b, Run run, SharedItem &it, int &each)
+{
+    constexpr int J = kEvenUnits / kWave;
+    const SharedGrid &g = a.s.grid;
+    const int lane = threadIdx.x & 63, units = a.s.L * a.s.Hkv * a.s.B;
+    const uint32_t step = 2 * (uint32_t)g.rows_t;
+    int n[J], off[J], tiles[J], end[J], most = 0;
+    float all = 0.f;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const int u = j * kWave + lane;
+        n[j] = off[j] = tiles[j] = 0;
+        if (j * kWave >= units) continue;
+        const int c = a.s.counts[min(u, units - 1)], s = min(u, units - 1) % a.s.B;
+        off[j] = a.s.offsets[min(u, units - 1)];
+        tiles[j] = g.tile0[s + 1] - g.tile0[s];
+        n[j] = u < units && c >= 0 && c <= a.s.max_count ? c : 0;
+        const int steps = (int)(((uint32_t)n[j] + step - 1) / step);
+        most = max(most, tiles[j] ? steps : 0);
+        all += (float)tiles[j] * (float)steps;
+    }
+    most = (int)wave_max_u32((uint32_t)most);
+    all = wave_sum(all);
+    const int hi = (most + a.even.least - 1) / a.even.least, lo = (most + g.np - 1) / g.np;
+    each = (int)fminf(ceilf(all / (float)a.even.fill), 1e9f);
+    each = uniform_i32(max(min(max(each, lo), hi), 1));
+    int total = 0;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        end[j] = total;
+        if (j * kWave >= units) continue;
+        const int steps = (int)(((uint32_t)n[j] + step - 1) / step);
+        end[j] += (int)wave_incl_scan((uint32_t)(tiles[j] * ((steps + each - 1) / each)));
+        total = __builtin_amdgcn_readlane(end[j], 63);
+    }
+    if (b >= (uint32_t)total) return false;
+    const int w = (int)run(b, (uint32_t)total);
+    int u = 0, rows = 0, before = 0;
+    bool found = false;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        if (found || j * kWave >= units) continue;
+        const unsigned long long m = __builtin_amdgcn_ballot_w64(end[j] > w);
+        if (m) {
+            const int i = __ffsll(m) - 1;
+            found = true;
+            u = j * kWave + i;
+            rows = __builtin_amdgcn_readlane(n[j], i);
+            it.base = __builtin_amdgcn_readlane(off[j], i);
+            const int steps = (int)(((uint32_t)rows + step - 1) / step);
+            before = __builtin_amdgcn_readlane(end[j], i) - __builtin_amdgcn_readlane(tiles[j], i) * ((steps + each - 1) / each);
+        }
+    }
+    const int lh = u / a.s.B, s = u - lh * a.s.B, per = g.tile0[s + 1] - g.tile0[s], r = w - before;
+    const int part = r / per, tile = r - part * per, qt = g.wq * g.rows_q;
+    it.c0 = a.s.fan[s];
+    it.nc = a.s.fan[s + 1] - it.c0;
+    it.q0 = tile * qt;
+    it.nq = min(qt, a.s.G * it.nc - it.q0);
+    it.l = lh / a.s.Hkv;
+    it.h = lh - it.l * a.s.Hkv;
+    it.part = part;
+    it.row0 = part * each * (int)step;
+    it.rows = min(rows - it.row0, each * (int)step);
+    return true;
+}
+
 // What lanes of a wave wrote to LDS before is what others read after.
 __device__ __forceinline__ void wave_lds_order()
 {
@@ -461,8 +532,11 @@ __global__ __launch_bounds__(kShThreads, 2) void k_tree(TreeArgs a)
     typedef ShGeo<BF, D, 16> Ge;
     __shared__ u32x4s lds[kShWaves * 2 * Ge::TILE];
     __shared__ TreeFlags flags[kShWaves];
-    const uint32_t b = blockIdx.z * (uint32_t)kGridX + blockIdx.x;
     const uint32_t prompts = (uint32_t)a.s.grid.prompt_blocks, padded = (prompts + kShXcds - 1) / kShXcds * kShXcds;
+    const uint32_t blocks = (uint32_t)a.tails.blocks;
+    // the prompts' blocks first, or the tails' (TreeEven)
+    const uint32_t b0 = blockIdx.z * (uint32_t)kGridX + blockIdx.x, ahead = a.even.ahead ? (blocks + kShXcds - 1) / kShXcds * kShXcds : 0;
+    const uint32_t b = b0 - ahead, tb = ahead ? b0 : b0 - padded;  // (past all of the prompts' in the tails' blocks ahead)
     // (each XCD takes a run of the work, in which the tiles of a part are neighbours)
     const auto run = [&](uint32_t b, uint32_t n) {
         const uint32_t x = b % kShXcds;
@@ -471,13 +545,19 @@ __global__ __launch_bounds__(kShThreads, 2) void k_tree(TreeArgs a)
     if (b < padded) {
         if (b >= prompts) return;
         SharedItem it;
-        prompt_item(a.s, run(b, prompts), it);
+        if (WQ == 4 && a.even.fill > 0) {
+            int each;
+            const bool there = even_item(a, b, run, it, each);
+            if (b == 0 && threadIdx.x == 0) a.s.part_steps[0] = each;
+            if (!there) return;
+        } else {
+            prompt_item(a.s, run(b, prompts), it);
+        }
         if (it.rows > 0) {
             if constexpr (WQ == 1) prompt_part<BF, D, 1, BF ? kTreeSummands : 3>(a.s, it, lds);
             else wide_prompt<BF, D>(a.s, it, lds);
         }
     } else {
-        const uint32_t tb = b - padded, blocks = (uint32_t)a.tails.blocks;
         if (tb >= blocks) return;
         TreeItem it;
         if constexpr (TWQ == 1) {
@@ -509,7 +589,7 @@ static void launch_tree(const TreeArgs &a, dim3 grid, hipStream_t st)
 hipError_t tree_launch(const TreeArgs &a, bool bf16, hipStream_t st)
 {
     const int64_t prompts = (a.s.grid.prompt_blocks + kShXcds - 1) / kShXcds * kShXcds;
-    const dim3 g = blocks_grid(prompts + a.tails.blocks);
+    const dim3 g = blocks_grid(prompts + (a.tails.blocks + kShXcds - 1) / kShXcds * kShXcds);
     if (bf16 && a.s.D == 128) ECOKV_TIMED("decode_tree", st, (launch_tree<true, 128>(a, g, st)));
     else if (bf16) ECOKV_TIMED("decode_tree", st, (launch_tree<true, 64>(a, g, st)));
     else if (a.s.D == 128) ECOKV_TIMED("decode_tree", st, (launch_tree<false, 128>(a, g, st)));

@@ -16,6 +16,21 @@ struct TreeTails {
     int64_t blocks;
 };
 
+// Several prompts' parts go by their counts, which the device alone knows (fill = 0:
+// they do not).  All blocks work out the same length of a part in steps of two tiles:
+// what gives about `fill` blocks, but between `least` and grid.np parts of the longest
+// unit.  The grid holds the most blocks that this can be.  Some then have nothing to do,
+// and the tails' blocks, which would wait for these, come first where their parts are
+// not short beside the prompts' (ahead).  (us, 13 nodes of 5, 1 and 6 continuations with
+// tails of 333 rows, 8 KV heads: equal parts, by counts, and the tails first: prompts of
+// 4480, 619 and 2610 rows 38.4 38.5 34.2, all of 4480 40.8 40.8 38.7; 38 heads of 4441 and
+// 2321 rows, 18 and 4 answers of 265 58.7 51.0 62.8.)
+struct TreeEven {
+    int least, fill, ahead;
+};
+constexpr int kEvenUnits = 256;   // at most: four of a lane
+constexpr size_t kEvenBytes = 16;  // of the workspace, behind the partials: a part's length
+
 // Rows of a prompt's part that are worth a block of its own, in wide and in narrow
 // tiles (us, 28 query rows of 4 heads, 1500 kept rows in parts of 768, 384 and 256: 15.7
 // 13.5 13.6; 6553 in parts of 640, 480 and 384: 15.5 14.7 14.3).
@@ -23,7 +38,7 @@ constexpr int kTreeRows = 512, kTreeNarrowRows = 256;
 
 // fan counts nodes (fan[s + 1] - fan[s] of prompt s); conts continuations.
 inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *fan, int conts, int nodes, int max_count,
-                            int max_tail, bool bf16, TreeTails *tails)
+                            int max_tail, bool bf16, TreeTails *tails, TreeEven *even)
 {
     SharedGrid g{};
     g.rows_q = g.rows_t = bf16 ? 32 : 16;
@@ -73,7 +88,6 @@ inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *f
         if (np > g.np) g.np = parts_within(np, max_count, g.step);
     }
     g.prompt_blocks = prompt_have * g.np;
-
     if (tails->wq == 1) {
         // waves: one for each SIMD, or two while their parts stay long
         g.tail_step = 2 * g.rows_t;
@@ -101,7 +115,16 @@ inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *f
     g.nt = parts_used(rows, g.nt, g.tail_step);  // (rounded up, fewer may do)
     g.tail_waves = tails->wq == 1 ? have * g.nt : 0;
     tails->blocks = tails->wq == 1 ? (g.tail_waves + kShWaves - 1) / kShWaves : have * g.nt;
-    g.bytes = sizeof(float) * (size_t)(g.np + g.nt) * (size_t)g.qrows * (size_t)(D + 2);
+    *even = TreeEven{0, 0, 0};
+    if (g.wq == 4 && g.np > 0 && prompts > 1 && pairs * B <= kEvenUnits && g.prompt_blocks + tails->blocks <= slots) {
+        const int64_t most = max_count / kTreeNarrowRows, twice = 2 * (int64_t)g.np;
+        even->least = g.np;
+        even->fill = (int)(slots - tails->blocks);
+        g.np = parts_within(most < g.np ? g.np : most < twice ? most : twice, max_count, g.step);
+        g.prompt_blocks = even->fill + prompt_have;
+        even->ahead = 3 * (int64_t)tails->rows * even->fill >= prompt_have * max_count;
+    }
+    g.bytes = sizeof(float) * (size_t)(g.np + g.nt) * (size_t)g.qrows * (size_t)(D + 2) + (even->fill ? kEvenBytes : 0);
     return g;
 }
 

@@ -35,11 +35,14 @@ static int covers(int n, int parts, int step) {
 extern "C" int tree(long long pairs, int G, int D, int B, const int *fan, int conts, int nodes, int max_count, int max_tail, int bf16, const int *n,
                     int nn, long long *out) {
     TreeTails t{};
-    const SharedGrid g = tree_grid(pairs, G, D, B, fan, conts, nodes, max_count, max_tail, bf16 != 0, &t);
+    TreeEven even{};
+    const SharedGrid g = tree_grid(pairs, G, D, B, fan, conts, nodes, max_count, max_tail, bf16 != 0, &t, &even);
     out[0] = g.np, out[1] = g.nt, out[2] = g.prompt_blocks, out[3] = t.blocks, out[4] = (long long)g.bytes, out[5] = t.rows;
+    out[6] = even.least, out[7] = even.fill, out[8] = 2 * g.rows_t;
+    for (int s = 0; s <= B; ++s) out[9 + s] = g.tile0[s];
     const int qt = g.wq * g.rows_q, tt = t.wq * g.rows_q;
     if ((g.wq != 1 && g.wq != 4) || (t.wq != 1 && t.wq != 4)) return 10;
-    if ((max_count > 0) != (g.np > 0) || g.prompt_blocks != pairs * g.tiles * g.np || g.step != g.rows_t * (kShWaves / g.wq)) return 11;
+    if ((max_count > 0) != (g.np > 0) || g.prompt_blocks != (even.fill ? even.fill + pairs * g.tiles : pairs * g.tiles * g.np) || g.step != g.rows_t * (kShWaves / g.wq)) return 11;
     for (int s = 0; s < B; ++s) {
         const long long M = (long long)G * (fan[s + 1] - fan[s]), k = g.tile0[s + 1] - g.tile0[s];
         if (k * qt < M || (M > 0 ? (k - 1) * qt >= M : k != 0)) return 12;
@@ -50,10 +53,11 @@ extern "C" int tree(long long pairs, int G, int D, int B, const int *fan, int co
     if (g.nt < 1 || t.rows < 1 || t.rows % g.tail_step || (long long)g.nt * t.rows < rows) return 14;
     const long long items = pairs * conts * t.tiles * g.nt;
     if (t.wq == 1 ? g.tail_waves != items || t.blocks != (items + kShWaves - 1) / kShWaves : t.blocks != items) return 15;
+    if (even.fill && (g.wq != 4 || even.least > g.np || even.fill < pairs * g.tiles * even.least || pairs * B > kEvenUnits)) return 17;
     for (int i = 0; i < nn; ++i)
         if (g.np > 0)
             if (int rc = covers(n[i] < max_count ? n[i] : max_count, g.np, g.step)) return rc;
-    return g.bytes == 4ull * (g.np + g.nt) * pairs * G * fan[B] * (D + 2) ? 0 : 16;
+    return g.bytes == 4ull * (g.np + g.nt) * pairs * G * fan[B] * (D + 2) + (even.fill ? kEvenBytes : 0) ? 0 : 16;
 }
 extern "C" int mass(long long pairs, int B, int conts, int max_count, int max_tail, long long *out) {
     int kp, tp;
@@ -85,11 +89,26 @@ def lib(tmp_path_factory):
     return lib
 
 
+def cover_by_counts(rng, out, pairs, B, max_count, kind):
+    """Parts by the counts: as the kernel works them out, every row of every tile is some block's, none past the grid or the workspace's places."""
+    parts, blocks, least, fill, step = (int(out[i]) for i in (0, 2, 6, 7, 8))
+    tiles = np.tile(np.diff(out[9:10 + B]), pairs).astype(np.int64)
+    n = [np.full(pairs * B, max_count), rng.integers(0, max_count + 1, pairs * B), np.zeros(pairs * B),
+         np.where(rng.random(pairs * B) < 0.1, max_count, 1)][kind].astype(np.int64)
+    steps = -(-n // step)
+    most = int((steps * (tiles > 0)).max())
+    want = int(np.ceil(np.float32((tiles * steps).sum()) / np.float32(fill)))
+    each = max(min(max(want, -(-most // parts)), -(-most // least)), 1)
+    used = -(-steps // each)
+    assert int((tiles * used).sum()) <= blocks and int((used * (tiles > 0)).max(initial=0)) <= parts
+    assert bool((used * each >= steps).all()) and bool(((used - 1) * each < np.maximum(steps, 1)).all())
+
+
 @pytest.mark.parametrize("G", [1, 2, 4, 7, 16, 64])
 @pytest.mark.parametrize("nodes", [1, 5, 16, 64])
 def test_tree_parts_cover_every_row_once(lib, G, nodes):
     rng = np.random.default_rng(G)
-    out = np.zeros(6, np.int64)
+    out = np.zeros(9 + 65, np.int64)
     for pairs in (1, 4, 32, 112, 900):
         for fan in ([1], [8], [0, 3], [5, 1, 12, 0, 3], [64], [1] * 64):
             conts = np.concatenate([[0], np.cumsum(fan)])
@@ -101,6 +120,9 @@ def test_tree_parts_cover_every_row_once(lib, G, nodes):
                     for D in (64, 128):
                         rc = lib.tree(pairs, G, D, len(fan), cum.ctypes.data, int(conts[-1]), nodes, mc, mt, bf16, n.ctypes.data, len(n), out.ctypes.data)
                         assert rc == 0, (rc, pairs, fan, mc, mt, bf16, D, out.tolist())
+                        if out[7] and (D == 128) == bool(bf16):
+                            for kind in range(4):
+                                cover_by_counts(rng, out, pairs, len(fan), mc, kind)
 
 
 def test_pieces_of_masses(lib):
