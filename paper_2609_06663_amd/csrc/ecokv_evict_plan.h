@@ -14,8 +14,8 @@ constexpr int kMassRows = 32;   // rows of a wave at a time
 // time.  Where there are more than kMassBlocks such pieces, it takes several of its
 // unit's, `parts` apart: the queries are listed and staged once for all of them.  (Us,
 // 28 layers of 6553 kept rows and four tails of 777, one query of each and accepted
-// paths: a piece a block 59.7 and 85.0, twice as many 50.1 and 76.7, 1536 blocks 49.0 and
-// 75.0, 768 blocks 55.3 and 82.7; 64 rows of a wave and 1536 blocks 55.4 and 78.6.)
+// paths: a piece a block 59.7 and 85.0, 1536 blocks 49.0 and 75.0, twice as many 50.1 and
+// 76.7, half as many 55.3 and 82.7; 64 rows of a wave and 1536 blocks 55.4 and 78.6.)
 constexpr int kMassBlocks = 1536;
 inline void mass_grid(int64_t pairs, int B, int conts, int max_count, int max_tail, int *kept_parts, int *tail_parts,
                       int64_t *kept_blocks, int64_t *tail_blocks)

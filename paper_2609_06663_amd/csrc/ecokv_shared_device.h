@@ -732,7 +732,8 @@ __global__ __launch_bounds__(kShMergeThreads) void k_shared_merge(SharedArgs a)
 // the four groups of them take every fourth partial, up to PER, all loaded at once, and
 // join by lane moves: an eighth of the loads of a lane of the forms above (us a whole
 // call, those forms and this: 1792 rows of 10 partials 28.2 26.9, 896 of 13 21.6 20.1,
-// 64-wide heads, 32 x 96 rows of 18, 66.2 63.6; of 6 to 8 partials 106.1 108.5, 111.7 112.7, 60.3 59.4).
+// 64-wide heads, 32 x 96 rows of 18, 66.2 63.6; of 6 to 8 partials 106.1 108.5, 111.7 112.7,
+// 60.3 59.4).
 template <int D, int PER>
 __global__ __launch_bounds__(kShMergeThreads) void k_shared_merge_wave(SharedArgs a)
 {
