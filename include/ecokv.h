@@ -565,9 +565,9 @@ int ecokv_decode_tree_workspace_size(const ecokv_shape *shape, const int32_t *fa
  * its continuation, a drafted row without one for the nodes that see it, a count out
  * of its bounds for the continuations concerned.
  * Arithmetic: logits, maxima, sums and accumulation in fp32.  With bf16 rows a weight
- * is rounded to bf16 where it multiplies a value (its own sum takes it unrounded), half
- * a step of 2^-8, as O is rounded to bf16 itself.  An infinity among the values of kept
- * rows or the tail's may give NaN in its dimension.
+ * multiplies a value as two bf16 summands, which leave out less than 2^-14 of it (its own
+ * sum takes it whole).  An infinity among the values of kept rows or the tail's may give
+ * NaN in its dimension.
  * Alignment, workspace and repeatability as ecokv_decode_shared; outputs and the
  * workspace overlap neither Q_dec nor the tails nor each other. */
 int ecokv_decode_tree(const void *Q_dec, const void *Kc, const void *Vc, int dtype, const ecokv_shape *shape,

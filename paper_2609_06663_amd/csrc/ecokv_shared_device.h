@@ -217,17 +217,12 @@ __device__ __forceinline__ void first_tile(const u32x4s *sk, typename ShGeo<BF, 
 }
 
 // The weights y0, y1 of two rows as dword j of the NS summands p.  Cut, not
-// rounded: what is left is exact, and the third summand the rest.  (The bf16 dot
+// rounded: what is left is exact, and the third summand the rest; two leave out less
+// than 2^-14 of the weight, a step of 2^-7 twice.  (The bf16 dot
 // instruction would take a fifth fewer, but not beside a matrix one.)
 template <int NS>
 __device__ __forceinline__ void cut_weights(float y0, float y1, u32x4s (&p)[NS], int j)
 {
-    if constexpr (NS == 1) {  // (one summand: rounded)
-        typedef __bf16 bf16x2s __attribute__((ext_vector_type(2)));
-        typedef float f32x2s __attribute__((ext_vector_type(2)));
-        p[0][j] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2s){y0, y1}, bf16x2s));
-        return;
-    }
 #pragma unroll
     for (int k = 0; k < NS; ++k) {
         p[k][j] = __builtin_amdgcn_perm(__float_as_uint(y1), __float_as_uint(y0), 0x07060302u);

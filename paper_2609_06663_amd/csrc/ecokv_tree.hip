@@ -20,12 +20,14 @@
 
 namespace ecokv {
 
-// bf16 summands of a weight in its product with bf16 values: one, rounded.  Its half
-// step of 2^-8 stands beside O's own; the weights' sum takes them unrounded.  (28
-// layers of 4 KV heads with 6553 rows, 8 continuations of 130 rows and 16 nodes, with
-// one, two and three: 469, 577 and 712 us; largest error against 64 bits, of values
-// around 1: 0.0023 with one, 0.0017 of a form whose O alone is rounded.)
-constexpr int kTreeSummands = 1;
+// bf16 summands of a weight in its product with bf16 values.  Two leave out less than
+// 2^-14 of it, and what is off in O is then O's own rounding, as for a weight of all its
+// bits; one, rounded, would be off by as much again.  Largest error against 64 bits,
+// relative, with one, two and three: 0.0023, 0.0017, 0.0017 (with O alone rounded 0.0017).
+// (us, the same: 64 nodes on 6553 kept rows of 4 heads 26.6 27.7 30.5; three prompts 34.4
+// 36.1 42.6; 64-wide tails of 8000 rows 63.9 64.4 65.8; 28 layers of 4 heads with 6553
+// rows, 8 continuations of 130 rows and 16 nodes, bound by matrix work, 445 560 690.)
+constexpr int kTreeSummands = 2;
 
 // Drafted rows of a part that need more than the loop does: no page there, or
 // values that are not finite; and whether a tail row has no page.
@@ -276,7 +278,7 @@ __device__ __forceinline__ void wide_part(const SharedArgs &a, const SharedItem 
         tile_reference<BF, D, QT>(fmaxf(mb[0], mb[1]), a.qscale, w);
         const float ref = w.m == -INFINITY ? 0.f : w.m;
         if constexpr (BF) {
-            u32x4s p[2][2][1];  // of tile h, rows 16 k ..
+            u32x4s p[2][2][kTreeSummands];  // of tile h, rows 16 k ..
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -290,7 +292,9 @@ __device__ __forceinline__ void wide_part(const SharedArgs &a, const SharedItem 
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int k = i / Ge::DT, d = i % Ge::DT, o = (2 * Ge::QS + i) % AHEAD;
-                w.acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[o], __builtin_bit_cast(bf16x8s, p[k / 2][k % 2][0]), w.acc[d], 0, 0, 0);
+#pragma unroll
+                for (int j = kTreeSummands - 1; j >= 0; --j)
+                    w.acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[o], __builtin_bit_cast(bf16x8s, p[k / 2][k % 2][j]), w.acc[d], 0, 0, 0);
                 if (i + AHEAD < NV) op[o] = vop(i + AHEAD);
                 __builtin_amdgcn_sched_barrier(0);
             }
