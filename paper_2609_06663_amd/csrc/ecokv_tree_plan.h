@@ -41,6 +41,9 @@ inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *f
                             int max_tail, bool bf16, TreeTails *tails, TreeEven *even)
 {
     SharedGrid g{};
+    *tails = TreeTails{};
+    *even = TreeEven{0, 0, 0};
+    if (pairs <= 0 || conts <= 0) return g;  // (no layers, or nobody continues)
     g.rows_q = g.rows_t = bf16 ? 32 : 16;
     int64_t most = 0, narrow_tiles = 0, prompts = 0;
     for (int s = 0; s < B; ++s) {
@@ -115,7 +118,6 @@ inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *f
     g.nt = parts_used(rows, g.nt, g.tail_step);  // (rounded up, fewer may do)
     g.tail_waves = tails->wq == 1 ? have * g.nt : 0;
     tails->blocks = tails->wq == 1 ? (g.tail_waves + kShWaves - 1) / kShWaves : have * g.nt;
-    *even = TreeEven{0, 0, 0};
     if (g.wq == 4 && g.np > 0 && prompts > 1 && pairs * B <= kEvenUnits && g.prompt_blocks + tails->blocks <= slots) {
         const int64_t most = max_count / kTreeNarrowRows, twice = 2 * (int64_t)g.np;
         even->least = g.np;
