@@ -179,7 +179,8 @@ class Continuations:
     The calls only enqueue work, on one stream at a time (they share a
     workspace): `advance` goes where the last `step` went, to the stream that it
     was given or else to the current one.  Who changes the stream between calls
-    orders the one after the other.  To capture them in a HIP graph, pass them
+    orders the one after the other, and keeps this and the pass until other streams
+    than the one it was made on have done their work.  To capture them in a HIP graph, pass them
     max_tail (max_new, or the limit's bound): by default it is the present length,
     which a replay would not raise.  A replay moves the device's counters only;
     `length`, the tails' rows or more, is the caller's to keep."""
@@ -230,6 +231,7 @@ class Continuations:
             need = max(need, E.ecokv_decode_tree_workspace_size(shape, self.fan, self.max_count, self.max_new, self.max_nodes))
         self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)
         self._outgrown = []  # workspaces that a captured graph may still use
+        self._captured = []  # trees that one reads
         # of drafts: of max_nodes nodes each, of fewer the beginning
         n = L * Hq * N * self.max_nodes
         self._nodes = torch.empty(n * D, dtype=dtype, device=dev), torch.empty(n * D, dtype=dtype, device=dev), torch.empty(n, device=dev)
@@ -302,8 +304,11 @@ class Continuations:
         self.lse_nodes = self._nodes[2][:n].view(L, Hq, N * M)
         self._need(E.ecokv_decode_tree_workspace_size(self.ep.shape, self.fan, self.max_count, max_tail, M), stream)
         self._stream = stream
+        tree._used_on(stream)
         with torch.cuda.stream(stream):  # (None: the current stream stays)
             rows, positions = self._at[0::2, :, None] + tree.steps
+            if tree.masks.is_cuda and torch.cuda.is_current_stream_capturing():
+                self._captured.append(tree)
         E.ecokv_append(Q, K, V, self.ep.shape, self.rope, positions, tree.conts, rows, self.tails, self.Q_nodes, stream)
         E.ecokv_decode_tree(self.Q_nodes, self.ep.Kc, self.ep.Vc, self.ep.shape, self.fan, self.ep.counts, self.ep.offsets, self.max_count,
                             self.tails, self.rows, max_tail, tree.masks, self.O_nodes, self.lse_nodes, self.workspace, stream)
@@ -322,6 +327,7 @@ class Continuations:
             raise ValueError(f"path has shape {tuple(path.shape)}, the draft has ({N}, {M}) nodes")
         stream = self._stream if stream is None else stream
         E.ecokv_commit(self.ep.shape, self.tails, self.rows, path, accepted, stream)
+        _used_on(stream, path, accepted)
         with torch.cuda.stream(stream):
             self._at.add_(accepted)
         self.length = self.length + M if longest is None else min(self.length + M, int(longest))
@@ -342,6 +348,8 @@ class Continuations:
         stream = self._stream if stream is None else stream
         E.ecokv_accumulate(Q, lse, self.ep.Kc, self.ep.shape, self.fan, self.ep.counts, self.ep.offsets, self.max_count, self.tails, counts,
                            most if max_tail is None else max_tail, self.mass, self.tail_mass, path, accepted, decay, stream=stream)
+        if path is not None:
+            _used_on(stream, path, accepted)
         self._unweighed = None
 
     def evict(self, limit: int, keep: int, recent: int, stream=None, max_tail: Optional[int] = None) -> None:
@@ -376,8 +384,17 @@ class Continuations:
             raise ValueError(f"a {self._pending} is not finished: rows are evicted between tokens")
 
 
+def _used_on(stream, *tensors: torch.Tensor) -> None:
+    """A call on `stream` (None: the current one) reads these: whoever drops them, their
+    memory is nobody else's before it has."""
+    for t in tensors:
+        if t.is_cuda:
+            t.record_stream(torch.cuda.current_stream(t.device) if stream is None else stream)
+
+
 class Tree:
-    """Drafted trees of continuations on the device (made by Continuations.tree)."""
+    """Drafted trees of continuations on the device (made by Continuations.tree).  A draft
+    that was enqueued does not need the Tree kept, nor does a captured one."""
 
     def __init__(self, parents, nodes: int, device):
         masks, steps = [], [[], []]  # (row behind the tail, depth)
@@ -391,3 +408,6 @@ class Tree:
         self.masks = torch.tensor(masks, dtype=torch.int64, device=device)
         self.steps = torch.tensor(steps, dtype=torch.int32, device=device)
         self.conts = torch.tensor([c for c in range(len(parents)) for _ in range(nodes)], dtype=torch.int32, device=device)
+
+    def _used_on(self, stream) -> None:
+        _used_on(stream, self.masks, self.steps, self.conts)
