@@ -656,7 +656,9 @@ int ecokv_evict(void *Kc, void *Vc, int dtype, const ecokv_shape *shape, const i
 
 /* The same for the tails: a continuation with more than `limit` rows keeps `keep`, every
  * (layer, KV head) its own.  new_counts: DEVICE [N], may be tail_counts.  Of the shape
- * num_layers, num_kv_heads and head_dim are read.  Positions go on as if nothing had gone.  A
+ * num_layers, num_kv_heads and head_dim are read.  Positions go on as if nothing had gone.
+ * Where tail_mass_out is tail_mass, the masses from row `keep` to the last that a tail had
+ * become 0, with which a row that is appended there and not accumulated begins.  A
  * continuation any of whose rows has no page in [0, num_pages) stays as it is; pages that are
  * written belong to one continuation alone. */
 int ecokv_evict_tails(int dtype, const ecokv_shape *shape, const ecokv_tails *tails, const int32_t *tail_counts,

@@ -454,6 +454,9 @@ __device__ __forceinline__ void move_masses(const EvictArgs &a, const EvictUnit 
         __syncthreads();  // (a place may be a row that another thread has yet to read)
         if (r < a.recent) a.mass_out[evict_at(a, x, heavy + r)] = m;
     }
+    // (a tail grows again: a row that comes to such a place begins with nothing)
+    if (a.tails && a.mass_out == a.mass)
+        for (int r = a.keep + t; r < n; r += kMoveThreads) a.mass_out[evict_at(a, x, r)] = 0.f;
 }
 
 // A block moves the chunks [c0, c0 + cols) of 16 bytes of a unit's rows, K's and V's

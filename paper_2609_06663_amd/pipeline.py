@@ -171,7 +171,8 @@ class Continuations:
     at once: `tree` lays out what sees what, `draft` takes the place of `step` and
     `commit` of `advance`, which adds to each tail the nodes that were accepted,
     as many as there are.  With `masses`, `accumulate` after a step or a commit
-    adds up what weight every row gets (`mass`, `tail_mass`), and between tokens
+    adds up what weight every row gets (`mass`, `tail_mass`; a row whose own step or
+    commit was not accumulated begins with 0), and between tokens
     `evict` bounds the tails and `evict_kept` the prompts' rows (of the pass
     itself) by dropping those of the least: with a limit below `max_new`
     generation need not end.
@@ -202,6 +203,7 @@ class Continuations:
         self._stream = None  # that the last step was given
         self._pending = None  # "step" or "draft": rows that are not the tails' yet
         self._unweighed = None  # "step", or the path of a commit: what accumulate may add
+        self._ahead = False  # whether the masses behind the tails hold those of a step that was not advanced
         self.fan = [0]
         for f in fan_out:
             self.fan.append(self.fan[-1] + f)
@@ -255,6 +257,7 @@ class Continuations:
         N = self.fan[-1]
         if isinstance(K, torch.Tensor) and K.shape[-3:-2] != (N,):  # (fewer would leave Q_dec laid out for fewer)
             raise ValueError(f"K has shape {tuple(K.shape)}, a step takes a token of each of the {N} continuations")
+        self._replace(stream)
         self._stream = stream
         E.ecokv_append(Q, K, V, self.ep.shape, self.rope, self.positions, None, self.rows, self.tails, self.Q_dec, stream)
         E.ecokv_decode_shared(self.Q_dec, self.ep.Kc, self.ep.Vc, self.ep.shape, self.fan, self.ep.counts, self.ep.offsets, self.max_count,
@@ -269,7 +272,7 @@ class Continuations:
             raise ValueError("a draft goes on with commit")
         with torch.cuda.stream(self._stream if stream is None else stream):  # (None: the current stream stays)
             self._at.add_(1)
-        self._pending = None
+        self._pending, self._ahead = None, False
         self.length += 1
 
     def tree(self, parents) -> "Tree":
@@ -303,6 +306,7 @@ class Continuations:
         self.Q_nodes, self.O_nodes = (t[:n * D].view(L, Hq, N * M, D) for t in self._nodes[:2])
         self.lse_nodes = self._nodes[2][:n].view(L, Hq, N * M)
         self._need(E.ecokv_decode_tree_workspace_size(self.ep.shape, self.fan, self.max_count, max_tail, M), stream)
+        self._replace(stream)
         self._stream = stream
         tree._used_on(stream)
         with torch.cuda.stream(stream):  # (None: the current stream stays)
@@ -350,7 +354,17 @@ class Continuations:
                            most if max_tail is None else max_tail, self.mass, self.tail_mass, path, accepted, decay, stream=stream)
         if path is not None:
             _used_on(stream, path, accepted)
-        self._unweighed = None
+        self._unweighed, self._ahead = None, self._pending == "step"
+
+    def _replace(self, stream) -> None:
+        """Another row takes the place of a step's that was weighed and not advanced."""
+        if self._ahead:
+            size = self.tails.K.shape[3]
+            with torch.cuda.stream(stream):
+                at = self.rows.long()
+                page = self.tails.table.long().gather(1, (at // size)[:, None])[:, 0]
+                self.tail_mass[:, page, :, at % size] = 0
+            self._ahead = False
 
     def evict(self, limit: int, keep: int, recent: int, stream=None, max_tail: Optional[int] = None) -> None:
         """Tails of more than `limit` rows keep `keep` of them: the last `recent`, and of
