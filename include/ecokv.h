@@ -530,7 +530,7 @@ int ecokv_decode_shared(const void *Q_dec, const void *Kc, const void *Vc, int d
  * values behind the tail (row tail_counts[c] + i, at the position after the tail's
  * last plus the node's depth), ecokv_decode_tree attends; then one ecokv_commit
  * over all layers puts the rows of the accepted path in order, and the caller adds
- * accepted[c] to the tail's rows and positions. */
+ * accepted[c] (or taken[c]) to the tail's rows and positions. */
 
 /* Host only: what each node of a tree sees.  parents (HOST [num_nodes]): -1, or an
  * earlier node.  masks (HOST [num_nodes]): bit j of masks[i] is set if node j is node
@@ -588,6 +588,12 @@ int ecokv_decode_tree(const void *Q_dec, const void *Kc, const void *Vc, int dty
  * continuation alone. */
 int ecokv_commit(int dtype, const ecokv_shape *shape, const ecokv_tails *tails, const int32_t *tail_counts,
                  int32_t num_nodes, const int32_t *path, const int32_t *accepted, void *stream);
+
+/* The same, and taken (DEVICE [N], overlapping none of the others) is how many rows each
+ * continuation's tail has more now: accepted[c], or 0 where it was left as it is.  (Nothing
+ * is written if there are no layers.) */
+int ecokv_commit_taken(int dtype, const ecokv_shape *shape, const ecokv_tails *tails, const int32_t *tail_counts,
+                       int32_t num_nodes, const int32_t *path, const int32_t *accepted, int32_t *taken, void *stream);
 
 /* ---- A cache that stays bounded while it generates ----
  *

@@ -1321,8 +1321,12 @@ int ecokv_decode_tree(const void *Q_dec, const void *Kc, const void *Vc, int dty
     return ECOKV_OK;
 }
 
-int ecokv_commit(int dtype, const ecokv_shape *shape, const ecokv_tails *tails, const int32_t *tail_counts,
-                 int32_t num_nodes, const int32_t *path, const int32_t *accepted, void *stream)
+}  // extern "C"
+
+namespace {
+
+int commit_impl(int dtype, const ecokv_shape *shape, const ecokv_tails *tails, const int32_t *tail_counts, int32_t num_nodes,
+                const int32_t *path, const int32_t *accepted, int32_t *taken, bool tells, void *stream)
 {
     ShapeInfo si;
     memset(&si, 0, sizeof si);
@@ -1339,6 +1343,11 @@ int ecokv_commit(int dtype, const ecokv_shape *shape, const ecokv_tails *tails, 
     if ((rc = check_tails(tails, si, es, &a.map, &tk, &tv))) return rc;
     if (overlap(tk, tv)) return fail(ECOKV_EINVAL, "the tails' K and V overlap");
     if (!tail_counts || !path || !accepted) return fail(ECOKV_EINVAL, "tail_counts, path and accepted must be non-NULL");
+    if (tells && !taken) return fail(ECOKV_EINVAL, "taken must be non-NULL");
+    const size_t n = 4 * (size_t)tails->num_conts;
+    const Span in[5] = {tk, tv, Span{tail_counts, n}, Span{path, n * num_nodes}, Span{accepted, n}};
+    for (int i = 0; tells && i < 5; ++i)
+        if (overlap(in[i], Span{taken, n})) return fail(ECOKV_EINVAL, "taken overlaps what the call reads or the tails");
     a.units = (int64_t)si.L * si.Hkv * tails->num_conts;
     if (a.units == 0) return ECOKV_OK;
     if (a.units > INT32_MAX / 4) return fail(ECOKV_EINVAL, "too many (layer, KV head, continuation) units");
@@ -1347,6 +1356,7 @@ int ecokv_commit(int dtype, const ecokv_shape *shape, const ecokv_tails *tails, 
     a.tail_counts = tail_counts;
     a.path = path;
     a.accepted = accepted;
+    a.taken = tells ? taken : nullptr;
     a.Hkv = si.Hkv;
     a.N = tails->num_conts;
     a.nodes = num_nodes;
@@ -1354,6 +1364,22 @@ int ecokv_commit(int dtype, const ecokv_shape *shape, const ecokv_tails *tails, 
     const hipError_t e = ecokv::commit_launch(a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "ecokv_commit launch");
     return ECOKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ecokv_commit(int dtype, const ecokv_shape *shape, const ecokv_tails *tails, const int32_t *tail_counts,
+                 int32_t num_nodes, const int32_t *path, const int32_t *accepted, void *stream)
+{
+    return commit_impl(dtype, shape, tails, tail_counts, num_nodes, path, accepted, nullptr, false, stream);
+}
+
+int ecokv_commit_taken(int dtype, const ecokv_shape *shape, const ecokv_tails *tails, const int32_t *tail_counts,
+                       int32_t num_nodes, const int32_t *path, const int32_t *accepted, int32_t *taken, void *stream)
+{
+    return commit_impl(dtype, shape, tails, tail_counts, num_nodes, path, accepted, taken, true, stream);
 }
 
 int ecokv_accumulate(const void *Q_dec, const float *lse, const void *Kc, int dtype, const ecokv_shape *shape,

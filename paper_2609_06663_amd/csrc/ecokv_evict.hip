@@ -35,7 +35,11 @@ __global__ __launch_bounds__(kCommitThreads) void k_commit(CommitArgs a)
     const int n = a.tail_counts[c], take = a.accepted[c];
     // lane k: from where to where the k-th accepted row goes
     const int path = a.path[(int64_t)c * a.nodes + min(lane, a.nodes - 1)];
-    if (n < 0 || take <= 0 || take > a.nodes) return;
+    const bool tells = a.taken && lh == 0 && lane == 0;  // what every unit of the continuation finds
+    if (n < 0 || take <= 0 || take > a.nodes) {
+        if (tells) a.taken[c] = 0;
+        return;
+    }
     const int node = lane < take ? path : a.nodes + lane;
     const int before = __shfl_up(node, 1, kWave);
     const int from = (int)((uint32_t)n + (uint32_t)node), to = (int)((uint32_t)n + (uint32_t)lane);
@@ -45,7 +49,9 @@ __global__ __launch_bounds__(kCommitThreads) void k_commit(CommitArgs a)
         pf = tail_page(a.map, c, from), pt = tail_page(a.map, c, to);
         good = node >= 0 && node < a.nodes && (lane == 0 || node > before) && pf >= 0 && pt >= 0;
     }
-    if (__builtin_amdgcn_ballot_w64(good) != ~0ull) return;
+    const bool whole = __builtin_amdgcn_ballot_w64(good) == ~0ull;
+    if (tells) a.taken[c] = whole ? take : 0;
+    if (!whole) return;
     const int stay = __popcll(__builtin_amdgcn_ballot_w64(node == lane));  // (the first ones: the nodes ascend)
     const int chunks = (take - stay) * S;
     constexpr int AT = 8;  // loads of each in a row

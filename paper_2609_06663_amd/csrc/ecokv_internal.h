@@ -295,6 +295,7 @@ hipError_t mass_launch(const MassArgs &a, bool bf16, hipStream_t st);
 struct CommitArgs {
     char *K, *V;
     const int32_t *tail_counts, *path, *accepted;
+    int32_t *taken;  // or NULL
     int Hkv, N, nodes, row_bytes;
     int64_t units;  // L Hkv N
     TailMap map;

@@ -40,7 +40,8 @@ EXPORTS = ["ecokv_default_params", "ecokv_workspace_size", "ecokv_workspace_stat
            "ecokv_decode_workspace_size", "ecokv_decode",
            "ecokv_rope_freqs", "ecokv_prefill_rope", "ecokv_append", "ecokv_decode_shared_workspace_size",
            "ecokv_decode_shared",
-           "ecokv_tree_masks", "ecokv_decode_tree_workspace_size", "ecokv_decode_tree", "ecokv_commit", "ecokv_accumulate",
+           "ecokv_tree_masks", "ecokv_decode_tree_workspace_size", "ecokv_decode_tree", "ecokv_commit", "ecokv_commit_taken",
+           "ecokv_accumulate",
            "ecokv_evict_workspace_size", "ecokv_evict", "ecokv_evict_tails",
            "ecokv_last_error", "ecokv_stage_times"]
 
@@ -249,6 +250,7 @@ def _load():
     lib.ecokv_decode_tree_workspace_size.argtypes = [sp, i32p, i32, i32, i32, ctypes.POINTER(sz)]
     lib.ecokv_decode_tree.argtypes = [vp, vp, vp, ctypes.c_int, sp, i32p, vp, vp, i32, tp, vp, i32, i32, vp, vp, vp, vp, sz, vp]
     lib.ecokv_commit.argtypes = [ctypes.c_int, sp, tp, vp, i32, vp, vp, vp]
+    lib.ecokv_commit_taken.argtypes = [ctypes.c_int, sp, tp, vp, i32, vp, vp, vp, vp]
     lib.ecokv_accumulate.argtypes = [vp, vp, vp, ctypes.c_int, sp, i32p, vp, vp, i32, tp, vp, i32, i32, vp, vp, ctypes.c_float,
                                      vp, vp, vp, vp, vp]
     lib.ecokv_evict_workspace_size.argtypes = [sp, i32, i32, i32, ctypes.POINTER(sz)]
@@ -869,9 +871,10 @@ def ecokv_decode_tree(Q_dec: torch.Tensor, Kc: Optional[torch.Tensor], Vc: Optio
 
 
 def ecokv_commit(shape: Shape, tails: Tails, tail_counts: torch.Tensor, path: torch.Tensor, accepted: torch.Tensor,
-                 stream=None) -> None:
+                 stream=None, taken: Optional[torch.Tensor] = None) -> None:
     """Enqueue ecokv_commit: row tail_counts[c] + path[c][k] to row tail_counts[c] + k,
-    k < accepted[c] (path: int32 [N][nodes])."""
+    k < accepted[c] (path: int32 [N][nodes]).  With `taken` (int32 [N]) ecokv_commit_taken:
+    the rows that each tail has more now, 0 where a path was refused."""
     c = shape.c
     if c.num_layers == 0:
         return
@@ -882,9 +885,10 @@ def ecokv_commit(shape: Shape, tails: Tails, tail_counts: torch.Tensor, path: to
     M = _per_node(path, "path", torch.int32, N, dev)
     if N == 0:
         return
-    _enqueue(lib.ecokv_commit, dev, stream, code, ctypes.byref(c), tails._arg(shape, dt, dev),
+    more = () if taken is None else (_fit(taken, "taken", torch.int32, N, dev),)
+    _enqueue(lib.ecokv_commit_taken if more else lib.ecokv_commit, dev, stream, code, ctypes.byref(c), tails._arg(shape, dt, dev),
              _fit(tail_counts, "tail_counts", torch.int32, N, dev), M, path.data_ptr(),
-             _fit(accepted, "accepted", torch.int32, N, dev))
+             _fit(accepted, "accepted", torch.int32, N, dev), *more)
 
 
 def ecokv_accumulate(Q_dec: torch.Tensor, lse: torch.Tensor, Kc: Optional[torch.Tensor], shape: Shape, fan: Sequence[int],

@@ -321,7 +321,8 @@ class Continuations:
 
     def commit(self, path: torch.Tensor, accepted: torch.Tensor, longest: Optional[int] = None, stream=None) -> None:
         """The accepted nodes of the draft become the tails' next rows: path int32
-        [N][nodes], of which the first accepted[c] (int32 [N]) count, ascending.
+        [N][nodes], of which the first accepted[c] (int32 [N]) count, ascending.  Of a
+        continuation with another path, or accepted[c] outside [0, nodes], none are.
         `longest`: the rows of the longest tail afterwards or more, where the caller
         knows better than `nodes` more than before."""
         if self._pending != "draft":
@@ -329,13 +330,19 @@ class Continuations:
         N, M = self.fan[-1], self.lse_nodes.shape[2] // self.fan[-1]
         if tuple(path.shape) != (N, M):
             raise ValueError(f"path has shape {tuple(path.shape)}, the draft has ({N}, {M}) nodes")
+        if not isinstance(accepted, torch.Tensor):
+            raise TypeError("accepted must be a torch tensor")
+        if tuple(accepted.shape) != (N,):
+            raise ValueError(f"accepted has shape {tuple(accepted.shape)}, the call needs ({N},)")
         stream = self._stream if stream is None else stream
-        E.ecokv_commit(self.ep.shape, self.tails, self.rows, path, accepted, stream)
+        with torch.cuda.stream(stream):
+            taken = accepted.clone()
+        E.ecokv_commit(self.ep.shape, self.tails, self.rows, path, accepted, stream, taken=taken)
         _used_on(stream, path, accepted)
         with torch.cuda.stream(stream):
-            self._at.add_(accepted)
+            self._at.add_(taken)
         self.length = self.length + M if longest is None else min(self.length + M, int(longest))
-        self._pending, self._unweighed = None, (path, accepted)
+        self._pending, self._unweighed = None, (path, taken)
 
     def accumulate(self, decay: float = 1.0, stream=None, max_tail: Optional[int] = None) -> None:
         """Add the weights of the last step, or of the accepted nodes of the last
