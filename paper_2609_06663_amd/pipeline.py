@@ -42,6 +42,7 @@ class EvictionPass:
         self.offsets = torch.empty(max(U, 1), dtype=torch.int32, device=device)
         self.Kc = torch.empty((max(self.n_idx, 1), D), dtype=dtype, device=device)
         self.Vc = torch.empty((max(self.n_idx, 1), D), dtype=dtype, device=device)
+        self.evictions = 0  # by Continuations, which move rows of Kc and Vc
 
     def score(self, K: torch.Tensor, Q_win: torch.Tensor, stream=None, V: Optional[torch.Tensor] = None,
               pre: Optional[torch.Tensor] = None):
@@ -240,6 +241,7 @@ class Continuations:
         self.Q_nodes = self.O_nodes = self.lse_nodes = None
         self.mass = self.tail_mass = None
         if masses:
+            self._evictions = ep.evictions
             self.mass = torch.zeros(ep.Kc.shape[0], dtype=torch.float32, device=dev)
             self.tail_mass = torch.zeros((L, N * per, Hkv, page_size), dtype=torch.float32, device=dev)
 
@@ -350,6 +352,7 @@ class Continuations:
         self._with_masses(False)
         if self._unweighed is None:
             raise ValueError("accumulate goes with a step or a commit, once")
+        self._with_order()
         if self._unweighed == "step":
             Q, lse, path, accepted = self.Q_dec, self.lse, None, None
         else:
@@ -388,8 +391,10 @@ class Continuations:
 
     def evict_kept(self, limit: int, keep: int, recent: int, stream=None) -> None:
         """The same for the prompts' kept rows, each (layer, KV head, prompt) on its own:
-        the pass's Kc, Vc and counts change."""
+        the pass's Kc, Vc and counts change, and other instances on it that have masses
+        can no longer accumulate or evict those."""
         self._with_masses(True)
+        self._with_order()
         shape = self.ep.shape
         stream = self._stream if stream is None else stream
         self._need(max(E.ecokv_evict_workspace_size(shape, shape.c.num_seqs, self.max_count, keep),
@@ -397,6 +402,11 @@ class Continuations:
         E.ecokv_evict(self.ep.Kc, self.ep.Vc, shape, self.ep.counts, self.ep.offsets, self.max_count, limit, keep, recent, self.mass,
                       workspace=self.workspace, stream=stream)
         self.max_count, self._unweighed = min(self.max_count, limit), None
+        self._evictions = self.ep.evictions = self.ep.evictions + 1
+
+    def _with_order(self) -> None:
+        if self._evictions != self.ep.evictions:
+            raise ValueError("another instance has moved the pass's rows since: `mass` is of their old order")
 
     def _with_masses(self, between: bool) -> None:
         if self.mass is None:
