@@ -259,9 +259,8 @@ class Continuations:
         N = self.fan[-1]
         if isinstance(K, torch.Tensor) and K.shape[-3:-2] != (N,):  # (fewer would leave Q_dec laid out for fewer)
             raise ValueError(f"K has shape {tuple(K.shape)}, a step takes a token of each of the {N} continuations")
-        self._replace(stream)
-        self._stream = stream
         E.ecokv_append(Q, K, V, self.ep.shape, self.rope, self.positions, None, self.rows, self.tails, self.Q_dec, stream)
+        self._appended(stream)
         E.ecokv_decode_shared(self.Q_dec, self.ep.Kc, self.ep.Vc, self.ep.shape, self.fan, self.ep.counts, self.ep.offsets, self.max_count,
                               self.tails, self.tail_counts, self.length + 1 if max_tail is None else max_tail, self.O, self.lse,
                               self.workspace, stream)
@@ -305,21 +304,20 @@ class Continuations:
             raise ValueError(f"K has shape {tuple(K.shape)}, the draft has {N} x {M} nodes")
         L, Hq, D = c.num_layers, c.num_q_heads, c.head_dim
         n, max_tail = L * Hq * N * M, self.length if max_tail is None else max_tail
-        self.Q_nodes, self.O_nodes = (t[:n * D].view(L, Hq, N * M, D) for t in self._nodes[:2])
-        self.lse_nodes = self._nodes[2][:n].view(L, Hq, N * M)
+        Q_nodes, O_nodes = (t[:n * D].view(L, Hq, N * M, D) for t in self._nodes[:2])
+        lse_nodes = self._nodes[2][:n].view(L, Hq, N * M)
         self._need(E.ecokv_decode_tree_workspace_size(self.ep.shape, self.fan, self.max_count, max_tail, M), stream)
-        self._replace(stream)
-        self._stream = stream
         tree._used_on(stream)
         with torch.cuda.stream(stream):  # (None: the current stream stays)
             rows, positions = self._at[0::2, :, None] + tree.steps
             if tree.masks.is_cuda and torch.cuda.is_current_stream_capturing():
                 self._captured.append(tree)
-        E.ecokv_append(Q, K, V, self.ep.shape, self.rope, positions, tree.conts, rows, self.tails, self.Q_nodes, stream)
-        E.ecokv_decode_tree(self.Q_nodes, self.ep.Kc, self.ep.Vc, self.ep.shape, self.fan, self.ep.counts, self.ep.offsets, self.max_count,
-                            self.tails, self.rows, max_tail, tree.masks, self.O_nodes, self.lse_nodes, self.workspace, stream)
-        self._pending, self._unweighed = "draft", None
-        return self.O_nodes
+        E.ecokv_append(Q, K, V, self.ep.shape, self.rope, positions, tree.conts, rows, self.tails, Q_nodes, stream)
+        self._appended(stream)
+        E.ecokv_decode_tree(Q_nodes, self.ep.Kc, self.ep.Vc, self.ep.shape, self.fan, self.ep.counts, self.ep.offsets, self.max_count,
+                            self.tails, self.rows, max_tail, tree.masks, O_nodes, lse_nodes, self.workspace, stream)
+        self.Q_nodes, self.O_nodes, self.lse_nodes, self._pending = Q_nodes, O_nodes, lse_nodes, "draft"
+        return O_nodes
 
     def commit(self, path: torch.Tensor, accepted: torch.Tensor, longest: Optional[int] = None, stream=None) -> None:
         """The accepted nodes of the draft become the tails' next rows: path int32
@@ -336,6 +334,7 @@ class Continuations:
             raise TypeError("accepted must be a torch tensor")
         if tuple(accepted.shape) != (N,):
             raise ValueError(f"accepted has shape {tuple(accepted.shape)}, the call needs ({N},)")
+        length = self.length + M if longest is None else min(self.length + M, int(longest))
         stream = self._stream if stream is None else stream
         with torch.cuda.stream(stream):
             taken = accepted.clone()
@@ -343,8 +342,7 @@ class Continuations:
         _used_on(stream, path, accepted)
         with torch.cuda.stream(stream):
             self._at.add_(taken)
-        self.length = self.length + M if longest is None else min(self.length + M, int(longest))
-        self._pending, self._unweighed = None, (path, taken)
+        self.length, self._pending, self._unweighed = length, None, (path, taken)
 
     def accumulate(self, decay: float = 1.0, stream=None, max_tail: Optional[int] = None) -> None:
         """Add the weights of the last step, or of the accepted nodes of the last
@@ -366,8 +364,11 @@ class Continuations:
             _used_on(stream, path, accepted)
         self._unweighed, self._ahead = None, self._pending == "step"
 
-    def _replace(self, stream) -> None:
-        """Another row takes the place of a step's that was weighed and not advanced."""
+    def _appended(self, stream) -> None:
+        """New queries and rows took the place of the last step's or draft's: what was not
+        advanced, committed or accumulated of these is gone, whatever comes of the new
+        ones, and a row of a step that was weighed and not advanced leaves no mass."""
+        self._stream, self._pending, self._unweighed = stream, None, None
         if self._ahead:
             size = self.tails.K.shape[3]
             with torch.cuda.stream(stream):
