@@ -246,11 +246,13 @@ class Continuations:
             self.tail_mass = torch.zeros((L, N * per, Hkv, page_size), dtype=torch.float32, device=dev)
 
     def _need(self, nbytes: int, stream) -> None:
-        """A workspace of nbytes (in order with `stream`, where it is given)."""
+        """A workspace of nbytes (in order with `stream`, where it is given).  One that is
+        too small makes way for one of twice its size at least: those that are kept are
+        smaller together than the last."""
         if self.workspace.numel() < nbytes:
             self._outgrown.append(self.workspace)
             with torch.cuda.stream(stream):  # (None: the current stream stays)
-                self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.workspace.device)
+                self.workspace = torch.empty(max(nbytes, 2 * self.workspace.numel()), dtype=torch.uint8, device=self.workspace.device)
 
     def step(self, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, stream=None, max_tail: Optional[int] = None) -> torch.Tensor:
         """Append the next token of every continuation and attend; returns O."""
