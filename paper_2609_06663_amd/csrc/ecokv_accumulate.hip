@@ -26,9 +26,10 @@ typedef float f32x4m __attribute__((ext_vector_type(4)));
 
 constexpr int kMassThreads = kMassWaves * kWave;
 constexpr int kMassList = 64 * 64;  // nodes that a block lists at a time: 64 continuations of 64
-// Tiles of 16 query rows staged at a time: six leave room for four blocks on a compute
-// unit and take 96 rows for all of a block's pieces at once (us, accepted paths of four
-// continuations, 28 layers: four tiles 74.6, six 56.4, eight 62.8).
+// Tiles of 16 query rows staged at a time: with rows of up to 256 bytes six leave room for
+// four blocks on a compute unit (34 KB of LDS each; with 512, fp32 of 128, 58 KB and two)
+// and take 96 rows for all of a block's pieces at once (us, accepted paths of four
+// continuations, 28 layers, bf16 of 128: four tiles 74.6, six 56.4, eight 62.8).
 constexpr int kMassTiles = 6;
 
 template <bool BF, int D>

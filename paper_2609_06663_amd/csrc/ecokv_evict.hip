@@ -548,6 +548,12 @@ hipError_t evict_launch(EvictArgs a, hipStream_t st)
         return dim3((unsigned)(n < kGridX ? n : kGridX), 1, (unsigned)((n + kGridX - 1) / kGridX));
     };
     const dim3 units = grid(a.units);
+    // A unit's keys stay in registers where they fit, 8 a thread, in the fewest threads: a
+    // rule on the bound, as the counts are the device's.  Past 8192 rows the masses are read
+    // again for each digit, also of units that have fewer.  (us a plan: 28 layers of 4 heads
+    // and 16 tails of 1152 rows, 256 and 1024 threads, 20.2 59.4; 4 units of 2048 rows 9.4
+    // 10.0; 4 units of 8192 rows under bounds of 8192 and 8193 13.7 25.3, 160 of up to 6553
+    // under 6553 and 26212 13.8 22.8; 4 of 16384 rows 42.1, of 26212 62.8.)
     if (a.max_rows <= 2048) ECOKV_TIMED("evict_plan", st, hipLaunchKernelGGL((k_evict_plan<256, 8>), units, dim3(256), 0, st, a));
     else if (a.max_rows <= 8192) ECOKV_TIMED("evict_plan", st, hipLaunchKernelGGL((k_evict_plan<1024, 8>), units, dim3(1024), 0, st, a));
     else ECOKV_TIMED("evict_plan", st, hipLaunchKernelGGL(k_evict_plan_long, units, dim3(kPlanThreads), 0, st, a));
