@@ -625,7 +625,8 @@ int ecokv_commit_taken(int dtype, const ecokv_shape *shape, const ecokv_tails *t
  * Only rows of the units and tails are read and written.  A prompt's or tail's rows are
  * left alone where its count is out of its bounds, and a tail row without a page is
  * skipped; a path's entry outside [0, num_nodes) adds nothing, nor does a query whose
- * lse is -inf; one whose lse is NaN gives NaN to the rows that it sees.  A page whose masses are kept belongs to one continuation alone.
+ * lse is -inf; one whose lse is NaN gives NaN to the rows that it sees.  A page whose
+ * masses are kept belongs to one continuation alone.
  * Arithmetic: fp32 (weights below 2^-126 count as 0).  The same call gives the same bits. */
 int ecokv_accumulate(const void *Q_dec, const float *lse, const void *Kc, int dtype, const ecokv_shape *shape,
                      const int32_t *fan, const int32_t *counts, const int32_t *offsets, int32_t max_count,
