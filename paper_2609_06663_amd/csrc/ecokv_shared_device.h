@@ -726,8 +726,8 @@ __global__ __launch_bounds__(kShMergeThreads) void k_shared_merge(SharedArgs a)
 // A tree's 9 to 32 partials: a wave per query row.  16 lanes share the row's D sums, and
 // the four groups of them take every fourth partial, up to PER, all loaded at once, and
 // join by lane moves: an eighth of the loads of a lane of the forms above (us a whole
-// call, those forms and this: 1792 rows of 10 partials 28.2 26.9, 896 of 13 21.6 20.1,
-// 64-wide heads, 32 x 96 rows of 18, 66.2 63.6; of 6 to 8 partials 106.1 108.5, 111.7 112.7,
+// call, those forms and this: 1792 rows of 10 partials 29.3 28.2, 896 of 13 21.8 20.1,
+// 64-wide heads, 32 x 96 rows of 18, 66.9 64.7; of 6 to 8 partials 106.1 108.5, 111.7 112.7,
 // 60.3 59.4).
 template <int D, int PER>
 __global__ __launch_bounds__(kShMergeThreads) void k_shared_merge_wave(SharedArgs a)
@@ -808,7 +808,7 @@ static hipError_t merge_launch(const SharedArgs &a, hipStream_t st)
     int per = few ? kShMergeThreads / (a.D / 4) : 1;
     if (TREE && parts > 5) {
         // (of so few rows a block each: us a whole call, the next form and this, 224 rows of 23
-        // partials 17.4 16.8, 112 of 30 15.1 14.5)
+        // partials 17.6 16.9, 112 of 30 15.6 14.7)
         if (a.grid.qrows <= 256 || parts > 32) few = 0, per = 1;
         else if (parts > 8) few = parts <= 16 ? 16 : 32, per = kShMergeThreads / kWave;
     }

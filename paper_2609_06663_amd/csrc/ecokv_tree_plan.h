@@ -23,8 +23,9 @@ struct TreeTails {
 // and the tails' blocks, which would wait for these, come first where their parts are
 // not short beside the prompts' (ahead).  (us, 13 nodes of 5, 1 and 6 continuations with
 // tails of 333 rows, 8 KV heads: equal parts, by counts, and the tails first: prompts of
-// 4480, 619 and 2610 rows 38.4 38.5 34.2, all of 4480 40.8 40.8 38.7; 38 heads of 4441 and
-// 2321 rows, 18 and 4 answers of 265 58.7 51.0 62.8.)
+// 4480, 619 and 2610 rows whose heads kept 6 to 14 tenths of them 44.9 39.8 36.0, three of
+// 4480 so kept 49.9 45.0 44.1, wholly kept 42.0 43.7 43.6; 38 64-wide heads of 4441 and 2321
+// rows, 18 and 4 answers of 265 68.7 59.6 74.7.)
 struct TreeEven {
     int least, fill, ahead;
 };
@@ -33,7 +34,7 @@ constexpr size_t kEvenBytes = 16;  // of the workspace, behind the partials: a p
 
 // Rows of a prompt's part that are worth a block of its own, in wide and in narrow
 // tiles (us, 28 query rows of 4 heads, 1500 kept rows in parts of 768, 384 and 256: 15.7
-// 13.5 13.6; 6553 in parts of 640, 480 and 384: 15.5 14.7 14.3).
+// 13.6 13.7; 6553 in parts of 640, 480 and 384: 15.5 14.7 14.5).
 constexpr int kTreeRows = 512, kTreeNarrowRows = 256;
 
 // fan counts nodes (fan[s + 1] - fan[s] of prompt s); conts continuations.
@@ -63,10 +64,10 @@ inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *f
     const int rows = max_tail + nodes;
     const int64_t short_parts = ((int64_t)rows + 4 * g.rows_t - 1) / (4 * g.rows_t);  // of four tiles
     // A wave of its own for query rows that fit one, but not with 128-wide bf16 rows: its
-    // loads, tile and sums need 61 registers more than there are (us, four waves and one:
-    // 28 query rows of 4 heads and 704 rows 15.5 23.7, 28 layers of them 91 109, 8 layers of
-    // 8000 rows 58 64; 128 heads of 24 query rows and 4000 rows 99 95; 64-wide, 1000 rows
-    // 23.4 21.6, 8000 rows 98 66; fp32 of 6 such answers, 28 layers, 1000 rows 154 96).
+    // loads, tile and sums need 62 registers more than there are (us, four waves and one:
+    // 28 query rows of 4 heads and 704 rows 14.7 23.6, 28 layers of them 87 110, 8 layers of
+    // 8000 rows 52 63; 128 heads of 24 query rows and 4000 rows 86 95; 64-wide, 1000 rows
+    // 25.0 20.7, 8000 rows 103 65; fp32 of 6 such answers, 28 layers, 1000 rows 154 96).
     tails->wq = nodes * G <= g.rows_q && !(bf16 && D == 128) ? 1 : 4;
     const int tt = tails->wq * g.rows_q;
     tails->tiles = (nodes * G + tt - 1) / tt;
@@ -78,7 +79,7 @@ inline SharedGrid tree_grid(int64_t pairs, int G, int D, int B, const int32_t *f
     if (g.wq == 1 && g.np > 0) {
         // no shorter parts, and no block that shares its compute unit with a tail's,
         // where that takes few parts away (us, 112 query rows of 4 heads, 6553 kept rows,
-        // 12 and 16 parts beside 24 blocks of tails: 20.0 22.6)
+        // 12 and 16 parts beside 24 blocks of tails: 20.2 23.0)
         const int64_t most = ((int64_t)max_count + kTreeNarrowRows - 1) / kTreeNarrowRows;
         const int64_t room = (kShBlocks - tail_least * short_parts) / prompt_have;
         int64_t np = g.np < most ? g.np : most;
