@@ -239,6 +239,7 @@ class Continuations:
         n = L * Hq * N * self.max_nodes
         self._nodes = torch.empty(n * D, dtype=dtype, device=dev), torch.empty(n * D, dtype=dtype, device=dev), torch.empty(n, device=dev)
         self.Q_nodes = self.O_nodes = self.lse_nodes = None
+        self._taken = torch.zeros(N, dtype=torch.int32, device=dev)  # by the last commit
         self.mass = self.tail_mass = None
         if masses:
             self._evictions = ep.evictions
@@ -339,12 +340,12 @@ class Continuations:
         length = self.length + M if longest is None else min(self.length + M, int(longest))
         stream = self._stream if stream is None else stream
         with torch.cuda.stream(stream):
-            taken = accepted.clone()
-        E.ecokv_commit(self.ep.shape, self.tails, self.rows, path, accepted, stream, taken=taken)
+            self._taken.copy_(accepted)
+        E.ecokv_commit(self.ep.shape, self.tails, self.rows, path, accepted, stream, taken=self._taken)
         _used_on(stream, path, accepted)
         with torch.cuda.stream(stream):
-            self._at.add_(taken)
-        self.length, self._pending, self._unweighed = length, None, (path, taken)
+            self._at.add_(self._taken)
+        self.length, self._pending, self._unweighed = length, None, (path, self._taken)
 
     def accumulate(self, decay: float = 1.0, stream=None, max_tail: Optional[int] = None) -> None:
         """Add the weights of the last step, or of the accepted nodes of the last
@@ -372,11 +373,14 @@ class Continuations:
         ones, and a row of a step that was weighed and not advanced leaves no mass."""
         self._stream, self._pending, self._unweighed = stream, None, None
         if self._ahead:
-            size = self.tails.K.shape[3]
+            table, pages, size = self.tails.table, *self.tails.K.shape[1:4:2]
             with torch.cuda.stream(stream):
-                at = self.rows.long()
-                page = self.tails.table.long().gather(1, (at // size)[:, None])[:, 0]
-                self.tail_mass[:, page, :, at % size] = 0
+                i = torch.arange(max(table.shape[1], size), device=table.device)
+                # the first row of each page that is behind its tail (of pages of nobody, none)
+                first = torch.full((pages + 1,), size, dtype=torch.int64, device=table.device)
+                page = torch.where((table >= 0) & (table < pages), table, pages).long()
+                first.scatter_(0, page.flatten(), (self.rows.long()[:, None] - size * i[:table.shape[1]]).flatten())
+                self.tail_mass.masked_fill_((i[:size] >= first[:pages, None])[None, :, None], 0)
             self._ahead = False
 
     def evict(self, limit: int, keep: int, recent: int, stream=None, max_tail: Optional[int] = None) -> None:
